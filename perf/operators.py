@@ -248,7 +248,7 @@ def _plain_append(s):
             x = x.float()
             # the least e with max|x| <= 448 * 2^e = 1.75 * 2^(8 + e)
             bits = x.abs().amax(2).contiguous().view(torch.int32)
-            e = (((bits + 0x1FFFFF) >> 23) - 135).clamp(min=-127)
+            e = (((bits + 0x1FFFFF) >> 23) - 135).clamp(min=-126)
             codes = torch.ldexp(x, -e[:, :, None]).to(torch.float8_e4m3fn)
             pages.view(torch.uint8)[p, :, o] = codes.view(torch.uint8)
             exps[p, :, o] = (e + 127).to(torch.uint8)
@@ -354,7 +354,7 @@ def exact(case, seed):
             if exps is not None:
                 # the values before their rounding to 8 bits
                 largest = x.abs().amax(2, keepdim=True)
-                e = torch.ceil(torch.log2(largest / 448)).clamp(min=-127)
+                e = torch.ceil(torch.log2(largest / 448)).clamp(min=-126)
                 e = torch.where(largest > 448 * torch.exp2(e), e + 1, e)
                 e = torch.where(largest <= 224 * torch.exp2(e), e - 1, e)
                 x = x * torch.exp2(-e)
