@@ -32,3 +32,12 @@ from .binding import (  # noqa: F401
     STRIDE,
     validate_index,
 )
+from . import paged  # noqa: F401, E402
+from .paged import (  # noqa: F401, E402
+    cache_append,
+    E4M3,
+    page_tables,
+    page_tables_workspace_bytes,
+    paged_attention,
+    paged_attention_workspace_bytes,
+)
