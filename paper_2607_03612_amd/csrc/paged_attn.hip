@@ -22,8 +22,12 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
+constexpr int kThreads = 256;
+constexpr int kCuCount = 256;
+// Waves of a launch, two to a SIMD: every wave takes the same number of tiles, at
+// least kMinTiles, so that a short launch does not spend itself on joining.
+constexpr int kWaves = kCuCount * 8;
+constexpr int kMinTiles = 2;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // kType: 0 fp32, 1 bf16, 2 e4m3.
@@ -40,12 +44,16 @@ struct Shape {
 };
 
 template <int kType, int kDim>
-struct Tile {
+struct KeyTile {
   using S = Shape<kType, kDim>;
-  uint32_t k[S::kGroups][S::kKWords];
-  uint32_t v[S::kGroups][4][S::kVWords];
-  uint32_t k_exp[S::kGroups];  // e4m3: of key lane % 16
-  uint32_t v_exp[S::kGroups];  // of keys 4g .. 4g + 3
+  uint32_t w[S::kGroups][S::kKWords];
+  uint32_t exp[S::kGroups];  // e4m3: of key lane % 16
+};
+template <int kType, int kDim>
+struct ValueTile {
+  using S = Shape<kType, kDim>;
+  uint32_t w[S::kGroups][4][S::kVWords];
+  uint32_t exp[S::kGroups];  // e4m3: of keys 4g .. 4g + 3
 };
 
 template <int kType, int kDim>
@@ -95,26 +103,35 @@ __device__ inline Span span_of(const DecodeArgs& a, int32_t length) {
   return s;
 }
 
-// A request's row of the table and a head of the pages.
-struct Source {
-  const int32_t* row;
-  const char* k;
-  const char* v;
-  const uint8_t* k_exp;
-  const uint8_t* v_exp;
-  int64_t exp_page;  // entries of a page's exponents
+// One tile of a request's row: what it is and where its keys lie.
+template <int kGroups>
+struct Place {
+  int32_t r;     // request
+  int32_t row;   // of its rows (key-value head, tile of query heads)
+  int32_t x;     // tile of the row, of s.count
+  int32_t tile;  // the same counted from the sequence's start
+  Span s;
+  int32_t page[kGroups];  // -1 for a page that holds no token or whose entry is no page
+  int64_t at[kGroups];    // bytes from a head's pages to the group's first key
+  int64_t exp[kGroups];   // entries to its exponents
 };
 
-// The pages of a tile's groups; -1 for one that holds no token or whose entry is
-// no page.
 template <int kGroups>
-__device__ inline void look_up(const DecodeArgs& a, const Source& src, const Span& s, int32_t tile, int32_t (&page)[kGroups]) {
+__device__ inline void look_up(const DecodeArgs& a, const int32_t* __restrict__ table, Place<kGroups>& p) {
+  p.tile = p.x < p.s.head ? p.x : p.x + p.s.skip;
+  const int h = p.row / a.qtiles;
 #pragma unroll
   for (int u = 0; u < kGroups; ++u) {
-    const int32_t pos = tile * (16 * kGroups) + 16 * u;
-    page[u] = -1;
-    if (pos < s.n) page[u] = src.row[div_page(a.page, pos)];
-    if (page[u] < 0 || page[u] >= a.pages) page[u] = -1;
+    const int32_t pos = p.tile * (16 * kGroups) + 16 * u;
+    const int32_t i = div_page(a.page, pos);
+    int32_t page = pos < p.s.n ? table[(int64_t)p.r * a.max_pages + i] : -1;
+    page = page < 0 || page >= a.pages ? -1 : page;
+    // an absent page's keys are read from page 0, which exists, and masked
+    const int32_t in = page < 0 ? 0 : pos - i * a.page.size;
+    const int64_t from = max(page, 0);
+    p.page[u] = page;
+    p.at[u] = from * a.page_stride + h * a.head_stride + (int64_t)in * a.token_stride;
+    p.exp[u] = (from * a.kv_heads + h) * a.page.size + in;
   }
 }
 
@@ -139,32 +156,33 @@ __device__ inline void load_words(uint32_t* to, const char* from) {
   }
 }
 
-// Reads stay inside pages: an absent page's keys are read from page 0 (which
-// exists) and masked, and so are the tokens of the last page behind the end.
+// Reads stay inside pages: a group's 16 keys lie in one page, whole.
 template <int kType, int kDim>
-__device__ inline void load_tile(const DecodeArgs& a, const Source& src, int32_t tile,
-                                 const int32_t (&page)[Shape<kType, kDim>::kGroups], Tile<kType, kDim>& t) {
+__device__ inline void load_keys(const DecodeArgs& a, const char* __restrict__ k, const uint8_t* __restrict__ exp,
+                                 const Place<Shape<kType, kDim>::kGroups>& p, KeyTile<kType, kDim>& t) {
   using S = Shape<kType, kDim>;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const uint32_t off = (uint32_t)(c * a.token_stride + g * 16);
 #pragma unroll
   for (int u = 0; u < S::kGroups; ++u) {
-    const int32_t pos = tile * S::kTile + 16 * u;
-    const int32_t p = max(page[u], 0);
-    const int32_t in = page[u] < 0 ? 0 : pos - div_page(a.page, pos) * a.page.size;
-    const int64_t at = p * a.page_stride + (int64_t)in * a.token_stride;
-    // K: row lane % 16, the pieces of 16 bytes g, g + 4, ...
-    const char* k = src.k + at + (uint32_t)(c * a.token_stride + g * 16);
+    // row lane % 16, the pieces of 16 bytes g, g + 4, ...
 #pragma unroll
-    for (int w = 0; w < S::kKWords / 4; ++w) load_words<4>(&t.k[u][4 * w], k + 64 * w);
-    // V: rows 4g .. 4g + 3, dimensions from (lane % 16) kDim / 16 on
+    for (int w = 0; w < S::kKWords / 4; ++w) load_words<4>(&t.w[u][4 * w], k + p.at[u] + off + 64 * w);
+    if constexpr (kType == 2) t.exp[u] = exp[p.exp[u] + c];
+  }
+}
+template <int kType, int kDim>
+__device__ inline void load_values(const DecodeArgs& a, const char* __restrict__ v, const uint8_t* __restrict__ exp,
+                                   const Place<Shape<kType, kDim>::kGroups>& p, ValueTile<kType, kDim>& t) {
+  using S = Shape<kType, kDim>;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const uint32_t off = (uint32_t)(4 * g * a.token_stride + c * (S::kVDims * S::kSize));
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      load_words<S::kVWords>(t.v[u][r], src.v + at + (uint32_t)((4 * g + r) * a.token_stride + c * (S::kVDims * S::kSize)));
-    if constexpr (kType == 2) {
-      const int64_t e = p * src.exp_page + in;
-      t.k_exp[u] = src.k_exp[e + c];
-      t.v_exp[u] = *reinterpret_cast<const uint32_t*>(src.v_exp + e + 4 * g);
-    }
+  for (int u = 0; u < S::kGroups; ++u) {
+    // rows 4g .. 4g + 3, dimensions from (lane % 16) kDim / 16 on
+#pragma unroll
+    for (int r = 0; r < 4; ++r) load_words<S::kVWords>(t.w[u][r], v + p.at[u] + (off + (uint32_t)(r * a.token_stride)));
+    if constexpr (kType == 2) t.exp[u] = *reinterpret_cast<const uint32_t*>(exp + p.exp[u] + 4 * g);
   }
 }
 
@@ -181,33 +199,29 @@ __device__ inline uint32_t bf16_pair(float x, float y) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
 }
 
-// One tile into the running softmax. With scores z in log2 units and the running
-// maximum m, every new maximum scales what is summed so far by 2^(m - m').
+// S^T of a tile.
 template <int kType, int kDim>
-__device__ inline void attend_tile(const DecodeArgs& a, const Span& s, int32_t tile,
-                                   const int32_t (&page)[Shape<kType, kDim>::kGroups], Tile<kType, kDim>& t,
-                                   const uint32_t (&q)[Shape<kType, kDim>::kQWords], State<kType, kDim>& st) {
+__device__ inline void score_tile(const KeyTile<kType, kDim>& t, const uint32_t (&q)[Shape<kType, kDim>::kQWords],
+                                  f32x4 (&z)[Shape<kType, kDim>::kGroups]) {
   using S = Shape<kType, kDim>;
-  const int g = (threadIdx.x & 63) >> 4;
-  f32x4 z[S::kGroups];
 #pragma unroll
   for (int u = 0; u < S::kGroups; ++u) {
     z[u] = f32x4{0, 0, 0, 0};
     if constexpr (kType == 0) {
 #pragma unroll
       for (int w = 0; w < kDim / 4; ++w)
-        z[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[u][w]), __uint_as_float(q[w]), z[u], 0, 0, 0);
+        z[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.w[u][w]), __uint_as_float(q[w]), z[u], 0, 0, 0);
     } else if constexpr (kType == 1) {
 #pragma unroll
       for (int w = 0; w < kDim / 32; ++w)
         z[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            as_bf16x8(t.k[u][4 * w], t.k[u][4 * w + 1], t.k[u][4 * w + 2], t.k[u][4 * w + 3]),
+            as_bf16x8(t.w[u][4 * w], t.w[u][4 * w + 1], t.w[u][4 * w + 2], t.w[u][4 * w + 3]),
             as_bf16x8(q[4 * w], q[4 * w + 1], q[4 * w + 2], q[4 * w + 3]), z[u], 0, 0, 0);
     } else {
-      const float scale = __uint_as_float(t.k_exp[u] << 23);
+      const float scale = __uint_as_float(t.exp[u] << 23);
 #pragma unroll
       for (int w = 0; w < kDim / 32; ++w) {
-        const uint32_t c0 = t.k[u][2 * w], c1 = t.k[u][2 * w + 1];
+        const uint32_t c0 = t.w[u][2 * w], c1 = t.w[u][2 * w + 1];
         z[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
             as_bf16x8(fp8_pair(c0, false, scale), fp8_pair(c0, true, scale), fp8_pair(c1, false, scale),
                       fp8_pair(c1, true, scale)),
@@ -215,24 +229,39 @@ __device__ inline void attend_tile(const DecodeArgs& a, const Span& s, int32_t t
       }
     }
   }
-  // tiles at an end of the kept tokens, or with an absent page: a masked key's
-  // score is -inf and its V row 0, whatever memory holds there
-  const int32_t first = tile * S::kTile, last = first + S::kTile;
-  bool whole = last <= s.n && (last <= s.anchor || first >= s.from);
+}
+
+// Tiles at an end of the kept tokens, or with an absent page: a masked key's
+// score is -inf and its V row 0, whatever memory holds there.
+template <int kGroups>
+__device__ inline bool is_whole(const Place<kGroups>& p) {
+  const int32_t first = p.tile * (16 * kGroups), last = first + 16 * kGroups;
+  bool whole = last <= p.s.n && (last <= p.s.anchor || first >= p.s.from);
 #pragma unroll
-  for (int u = 0; u < S::kGroups; ++u) whole = whole && page[u] >= 0;
-  if (!whole) {
+  for (int u = 0; u < kGroups; ++u) whole = whole && p.page[u] >= 0;
+  return whole;
+}
+
+// A tile's scores and V into the running softmax. With scores z in log2 units and
+// the running maximum m, every new maximum scales what is summed so far by 2^(m - m').
+template <int kType, int kDim>
+__device__ inline void add_tile(const DecodeArgs& a, const Place<Shape<kType, kDim>::kGroups>& pl, f32x4 (&z)[Shape<kType, kDim>::kGroups],
+                                ValueTile<kType, kDim>& t, State<kType, kDim>& st) {
+  using S = Shape<kType, kDim>;
+  const int g = (threadIdx.x & 63) >> 4;
+  if (!is_whole(pl)) {
+    const int32_t first = pl.tile * S::kTile;
 #pragma unroll
     for (int u = 0; u < S::kGroups; ++u)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int32_t j = first + 16 * u + 4 * g + r;
-        const bool keep = page[u] >= 0 && j < s.n && (j < s.anchor || j >= s.from);
+        const bool keep = pl.page[u] >= 0 && j < pl.s.n && (j < pl.s.anchor || j >= pl.s.from);
         if (!keep) {
           z[u][r] = -INFINITY;
 #pragma unroll
-          for (int w = 0; w < S::kVWords; ++w) t.v[u][r][w] = 0;
-          if constexpr (kType == 2) t.v_exp[u] = (t.v_exp[u] & ~(0xffu << (8 * r))) | 1u << (8 * r);
+          for (int w = 0; w < S::kVWords; ++w) t.w[u][r][w] = 0;
+          if constexpr (kType == 2) t.exp[u] = (t.exp[u] & ~(0xffu << (8 * r))) | 1u << (8 * r);
         }
       }
   }
@@ -265,7 +294,7 @@ __device__ inline void attend_tile(const DecodeArgs& a, const Span& s, int32_t t
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int i = 0; i < S::kVDims; ++i)
-          st.o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[u][r][i]), p[u][r], st.o[i], 0, 0, 0);
+          st.o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.w[u][r][i]), p[u][r], st.o[i], 0, 0, 0);
   } else {
 #pragma unroll
     for (int u = 0; u < S::kGroups; u += 2) {
@@ -286,10 +315,10 @@ __device__ inline void attend_tile(const DecodeArgs& a, const Span& s, int32_t t
 #pragma unroll
         for (int w = 0; w < S::kVDims / 2; ++w) {
           if constexpr (kType == 1) {
-            vw[x][w] = t.v[u + (x >> 2)][x & 3][w];
+            vw[x][w] = t.w[u + (x >> 2)][x & 3][w];
           } else {
-            const float scale = __uint_as_float(((t.v_exp[u + (x >> 2)] >> (8 * (x & 3))) & 0xffu) << 23);
-            vw[x][w] = fp8_pair(t.v[u + (x >> 2)][x & 3][w >> 1], w & 1, scale);
+            const float scale = __uint_as_float(((t.exp[u + (x >> 2)] >> (8 * (x & 3))) & 0xffu) << 23);
+            vw[x][w] = fp8_pair(t.w[u + (x >> 2)][x & 3][w >> 1], w & 1, scale);
           }
         }
 #pragma unroll
@@ -309,9 +338,11 @@ __device__ inline void attend_tile(const DecodeArgs& a, const Span& s, int32_t t
 // The queries of a tile of 16 heads: lane % 16 is the query, the pieces of its
 // row those of K's rows. Heads past the group are zeros.
 template <int kType, int kDim>
-__device__ inline void load_queries(const DecodeArgs& a, const char* q, int r, int first, int heads,
+__device__ inline void load_queries(const DecodeArgs& a, const char* __restrict__ q, int r, int row,
                                     uint32_t (&w)[Shape<kType, kDim>::kQWords]) {
   using S = Shape<kType, kDim>;
+  const int qt = row % a.qtiles, first = row / a.qtiles * a.group + 16 * qt;
+  const int heads = min(a.group - 16 * qt, 16);
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   constexpr int kIn = kType == 0 ? 4 : 2;
 #pragma unroll
@@ -332,125 +363,290 @@ __device__ inline void load_queries(const DecodeArgs& a, const char* q, int r, i
   }
 }
 
-template <int kType, int kDim>
-struct Merge {
-  static constexpr int kRow = kDim + 4;  // floats of a query's row in LDS
-  float o[kWaves][16][kRow];
-  float m[kWaves][16];
-  float l[kWaves][16];
+// Where a launch's pieces go: a row that falls to several waves leaves a part in
+// each, wave w's in slot 2w if the row began before the wave's tiles and in slot
+// 2w + 1 if it begins among them. Each part: kDim sums per query, and (m, l).
+struct Pieces {
+  float* o;    // [2 kWaves][heads][kDim]
+  float2* ml;  // [2 kWaves][heads]
+  int4* cut;   // a row that starts in wave w and ends in a later one: (request, row, w, last wave), else w < 0
 };
+constexpr int64_t kCutBytes = (int64_t)kWaves * sizeof(int4);
 
+__host__ __device__ inline Pieces pieces(void* workspace, int heads) {
+  Pieces p;
+  p.cut = static_cast<int4*>(workspace);
+  p.ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + kCutBytes);
+  p.o = reinterpret_cast<float*>(p.ml + 2 * kWaves * heads);
+  return p;
+}
+__host__ __device__ inline int piece_heads(const DecodeArgs& a) { return a.group < 16 ? a.group : 16; }
+
+// A wave's part of a row: the output where it has the whole row, else a piece.
 template <int kType, int kDim>
-__device__ inline void put_state(Merge<kType, kDim>& lds, int wave, const State<kType, kDim>& st) {
+__device__ inline void put_row(const DecodeArgs& a, const State<kType, kDim>& st, int r, int row, int slot, char* __restrict__ out,
+                               float* __restrict__ lse, const Pieces& pc) {
   using S = Shape<kType, kDim>;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const int qt = row % a.qtiles, first = row / a.qtiles * a.group + 16 * qt;
+  const int heads = min(a.group - 16 * qt, 16);
   const float l = across_groups_sum(st.l);
-  if (g == 0) {
-    lds.m[wave][c] = st.m;
-    lds.l[wave][c] = l;
+  if (c >= heads) return;
+  if (slot >= 0) {
+    const int at = slot * piece_heads(a) + c;
+    if (g == 0) pc.ml[at] = float2{st.m, l};
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int i = 0; i < S::kVDims; i += 4)
+        *reinterpret_cast<f32x4*>(pc.o + (int64_t)at * kDim + (4 * g + x) * S::kVDims + i) =
+            f32x4{st.o[i][x], st.o[i + 1][x], st.o[i + 2][x], st.o[i + 3][x]};
+    return;
   }
+  const float f = l > 0.0f ? 1.0f / l : l;  // 0 and NaN stay
+  const int head = first + c;
+  const int64_t at = head * a.out_head + r * a.out_request;
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
+  for (int x = 0; x < 4; ++x)
 #pragma unroll
-    for (int i = 0; i < S::kVDims; i += 4)
-      *reinterpret_cast<f32x4*>(&lds.o[wave][c][(4 * g + r) * S::kVDims + i]) =
-          f32x4{st.o[i][r], st.o[i + 1][r], st.o[i + 2][r], st.o[i + 3][r]};
+    for (int i = 0; i < S::kVDims; i += 4) {
+      const int64_t to = at + (4 * g + x) * S::kVDims + i;
+      const f32x4 y = f32x4{st.o[i][x], st.o[i + 1][x], st.o[i + 2][x], st.o[i + 3][x]} * f;
+      if constexpr (kType == 0)
+        *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + to) = y;
+      else
+        *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(out) + to) = u32x2{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])};
+    }
+  if (lse && g == 0) lse[(int64_t)head * a.requests + r] = (st.m + __log2f(l)) * kLn2;
 }
 
-// The outputs of one thread: kDim / 16 dimensions of query threadIdx.x / 16.
-template <int kType, int kDim>
-__device__ inline void put_output(const DecodeArgs& a, char* out, float* lse, int r, int head, const float* o, float m, float l) {
-  constexpr int kVDims = kDim / 16;
-  const float f = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // NaN stays
-  const int64_t at = head * a.out_head + r * a.out_request + (threadIdx.x & 15) * kVDims;
-  if constexpr (kType == 0) {
-    float* to = reinterpret_cast<float*>(out) + at;
-#pragma unroll
-    for (int i = 0; i < kVDims; i += 4) *reinterpret_cast<f32x4*>(to + i) = f32x4{o[i] * f, o[i + 1] * f, o[i + 2] * f, o[i + 3] * f};
-  } else {
-    uint32_t* to = reinterpret_cast<uint32_t*>(reinterpret_cast<uint16_t*>(out) + at);
-#pragma unroll
-    for (int i = 0; i < kVDims; i += 4)
-      *reinterpret_cast<u32x2*>(to + i / 2) = u32x2{bf16_pair(o[i] * f, o[i + 1] * f), bf16_pair(o[i + 2] * f, o[i + 3] * f)};
+// The next request after r that has tiles (64 lengths at a time), or `requests`.
+template <int kTile>
+__device__ inline int next_request(const DecodeArgs& a, const int32_t* __restrict__ lengths, int r) {
+  const int lane = threadIdx.x & 63;
+  for (++r; r < a.requests; r += 64) {
+    const bool some = r + lane < a.requests && lengths[r + lane] > 0;
+    const uint64_t found = __ballot(some);
+    if (found) return r + __ffsll((unsigned long long)found) - 1;
   }
-  if (lse && (threadIdx.x & 15) == 0) lse[(int64_t)head * a.requests + r] = (m + __log2f(l)) * kLn2;
+  return a.requests;
 }
 
-// One workgroup per request, key-value head and tile of its query heads; its
-// four waves take the tiles in turn.
+// The tiles of all requests' rows, request by request and row by row, are dealt
+// out to the waves in equal runs of neighbouring tiles. A wave goes through its
+// run without a stop: while it works on one tile's scores the next one's K is on
+// the way, while it works on V the next V.
 template <int kType, int kDim>
 __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
     const char* __restrict__ q, const char* __restrict__ k, const char* __restrict__ v,
     const uint8_t* __restrict__ k_exp, const uint8_t* __restrict__ v_exp, const int32_t* __restrict__ table,
-    const int32_t* __restrict__ lengths, char* __restrict__ out, float* __restrict__ lse, DecodeArgs a) {
+    const int32_t* __restrict__ lengths, char* __restrict__ out, float* __restrict__ lse, void* __restrict__ workspace,
+    DecodeArgs a) {
   using S = Shape<kType, kDim>;
-  __shared__ Merge<kType, kDim> lds;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int qt = blockIdx.x % a.qtiles;
-  const int h = blockIdx.x / a.qtiles % a.kv_heads;
-  const int r = blockIdx.x / a.qtiles / a.kv_heads;
-  const int heads = min(a.group - 16 * qt, 16), first = h * a.group + 16 * qt;
-  Source src;
-  src.row = table + (int64_t)r * a.max_pages;
-  src.k = k + h * a.head_stride;
-  src.v = v + h * a.head_stride;
-  src.exp_page = (int64_t)a.kv_heads * a.page.size;
-  src.k_exp = k_exp + h * a.page.size;
-  src.v_exp = v_exp + h * a.page.size;
-  const Span s = span_of<S::kTile>(a, lengths[r]);
-  uint32_t qw[S::kQWords];
-  load_queries<kType, kDim>(a, q, r, first, heads, qw);
-  State<kType, kDim> st;
-  st.m = -INFINITY;
-  st.l = 0.0f;
-#pragma unroll
-  for (int i = 0; i < S::kVDims; ++i) st.o[i] = f32x4{0, 0, 0, 0};
-  for (int32_t x = wave; x < s.count; x += kWaves) {
-    const int32_t tile = x < s.head ? x : x + s.skip;
-    int32_t page[S::kGroups];
-    Tile<kType, kDim> t;
-    look_up<S::kGroups>(a, src, s, tile, page);
-    load_tile<kType, kDim>(a, src, tile, page, t);
-    attend_tile<kType, kDim>(a, s, tile, page, t, qw, st);
+  __shared__ int64_t before[kThreads + 1];  // tiles of the requests before a thread's
+  __shared__ int64_t wave_sum[kThreads / 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = a.kv_heads * a.qtiles;
+  const Pieces pc = pieces(workspace, piece_heads(a));
+
+  // requests without a token
+  for (int r = blockIdx.x; r < a.requests; r += gridDim.x) {
+    if (lengths[r] > 0) continue;
+    for (int i = threadIdx.x; i < a.q_heads * (kDim / 4); i += kThreads) {
+      const int head = i / (kDim / 4), d = i % (kDim / 4) * 4;
+      const int64_t at = head * a.out_head + r * a.out_request + d;
+      if constexpr (kType == 0)
+        *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + at) = f32x4{0, 0, 0, 0};
+      else
+        *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(out) + at) = u32x2{0, 0};
+      if (lse && d == 0) lse[(int64_t)head * a.requests + r] = -INFINITY;
+    }
   }
-  put_state<kType, kDim>(lds, wave, st);
+
+  // where the runs lie: each thread counts neighbouring requests
+  const int each = (a.requests + kThreads - 1) / kThreads;
+  int64_t mine = 0;
+  for (int i = 0; i < each; ++i) {
+    const int r = threadIdx.x * each + i;
+    if (r < a.requests) mine += span_of<S::kTile>(a, lengths[r]).count;
+  }
+  mine *= rows;
+  int64_t sum = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(sum, d);
+    if (lane >= d) sum += y;
+  }
+  if (lane == 63) wave_sum[wave] = sum;
   __syncthreads();
-  const int query = threadIdx.x >> 4, part = threadIdx.x & 15;
-  if (query >= heads) return;
-  float m = -INFINITY;
+  int64_t total = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, lds.m[w][query]);
-  float l = 0.0f, o[S::kVDims] = {};
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const float f = lds.m[w][query] == -INFINITY ? 0.0f : exp2_fast(lds.m[w][query] - m);
-    l = fmaf(lds.l[w][query], f, l);
-#pragma unroll
-    for (int i = 0; i < S::kVDims; ++i) o[i] = fmaf(lds.o[w][query][part * S::kVDims + i], f, o[i]);
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w == wave) sum += total;
+    total += wave_sum[w];
   }
-  put_output<kType, kDim>(a, out, lse, r, first + query, o, m, l);
+  before[threadIdx.x] = sum - mine;
+  __syncthreads();
+
+  const int64_t run = max((total + kWaves - 1) / kWaves, (int64_t)kMinTiles);
+  const int w = wave * gridDim.x + blockIdx.x;  // neighbouring runs on different CUs
+  const int64_t lo = w * run, hi = min(lo + run, total);
+  if (lane == 0) pc.cut[w].z = -1;
+  if (lo >= hi) return;
+
+  // the first tile's request: the thread whose requests hold it, then these one by one
+  int owner = 0;
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) owner += __popcll(__ballot(before[64 * i + lane] <= lo));
+  owner -= 1;
+  Place<S::kGroups> next;
+  next.r = owner * each;
+  int64_t off = lo - before[owner];
+  next.s = span_of<S::kTile>(a, lengths[next.r]);
+  while (off >= (int64_t)next.s.count * rows) {
+    off -= (int64_t)next.s.count * rows;
+    next.s = span_of<S::kTile>(a, lengths[++next.r]);
+  }
+  next.r = __builtin_amdgcn_readfirstlane(next.r);
+  next.s = span_of<S::kTile>(a, lengths[next.r]);
+  next.row = (int32_t)(off / next.s.count);
+  next.row = __builtin_amdgcn_readfirstlane(next.row);
+  next.x = __builtin_amdgcn_readfirstlane((int32_t)(off - (int64_t)next.row * next.s.count));
+
+  KeyTile<kType, kDim> kt;
+  ValueTile<kType, kDim> vt;
+  State<kType, kDim> st;
+  uint32_t qw[S::kQWords], qn[S::kQWords];
+  look_up<S::kGroups>(a, table, next);
+  load_queries<kType, kDim>(a, q, next.r, next.row, qn);
+  load_keys<kType, kDim>(a, k, k_exp, next, kt);
+  load_values<kType, kDim>(a, v, v_exp, next, vt);
+  bool begins = true;         // the tile is the wave's first of its row
+  bool from_start = next.x == 0;  // and the row's first
+  int64_t left = hi - lo;
+  while (true) {
+    const Place<S::kGroups> now = next;
+    if (begins) {
+#pragma unroll
+      for (int i = 0; i < S::kQWords; ++i) qw[i] = qn[i];
+      st.m = -INFINITY;
+      st.l = 0.0f;
+#pragma unroll
+      for (int i = 0; i < S::kVDims; ++i) st.o[i] = f32x4{0, 0, 0, 0};
+      from_start = now.x == 0;
+    }
+    f32x4 z[S::kGroups];
+    score_tile<kType, kDim>(kt, qw, z);
+    const bool ends = now.x + 1 == now.s.count;
+    --left;
+    if (left > 0) {
+      if (!ends) {
+        ++next.x;
+      } else {
+        next.x = 0;
+        if (++next.row == rows) {
+          next.row = 0;
+          next.r = __builtin_amdgcn_readfirstlane(next_request<S::kTile>(a, lengths, next.r));
+          next.s = span_of<S::kTile>(a, lengths[next.r]);
+        }
+        load_queries<kType, kDim>(a, q, next.r, next.row, qn);
+      }
+      look_up<S::kGroups>(a, table, next);
+      load_keys<kType, kDim>(a, k, k_exp, next, kt);
+    }
+    add_tile<kType, kDim>(a, now, z, vt, st);
+    if (left > 0) load_values<kType, kDim>(a, v, v_exp, next, vt);
+    begins = ends;
+    if (ends || left == 0) {
+      const bool whole = ends && from_start;
+      put_row<kType, kDim>(a, st, now.r, now.row, whole ? -1 : from_start ? 2 * w + 1 : 2 * w, out, lse, pc);
+      if (!ends && from_start && lane == 0) {
+        // tiles of the row behind this run, a run each wave
+        const int64_t behind = now.s.count - 1 - now.x;
+        pc.cut[w] = int4{now.r, now.row, w, w + (int)((behind + run - 1) / run)};
+      }
+    }
+    if (left == 0) break;
+  }
+}
+
+// The rows that fell to several waves: one workgroup per such row and query, its
+// 16-byte lanes spread over kThreads * 4 / kDim pieces at a time, in the order of
+// the waves.
+template <int kType, int kDim>
+__global__ __launch_bounds__(kThreads) void paged_join_kernel(const void* __restrict__ workspace, char* __restrict__ out,
+                                                              float* __restrict__ lse, DecodeArgs a) {
+  constexpr int kLanes = kDim / 4, kAtOnce = kThreads / kLanes;
+  __shared__ f32x4 part[kAtOnce][kLanes];
+  __shared__ float2 part_ml[kAtOnce];
+  const Pieces pc = pieces(const_cast<void*>(workspace), piece_heads(a));
+  const int4 cut = pc.cut[blockIdx.x];
+  if (cut.z < 0) return;
+  const int qt = cut.y % a.qtiles, n = blockIdx.y;
+  if (n >= min(a.group - 16 * qt, 16)) return;
+  const int head = cut.y / a.qtiles * a.group + 16 * qt + n;
+  const int slot = threadIdx.x / kLanes, d = threadIdx.x % kLanes;
+  const int count = cut.w - cut.z + 1;
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o{0, 0, 0, 0};
+  for (int i = slot; i < count; i += kAtOnce) {
+    const int at = (2 * (cut.z + i) + (i == 0 ? 1 : 0)) * piece_heads(a) + n;
+    const float2 ml = pc.ml[at];
+    const f32x4 x = *reinterpret_cast<const f32x4*>(pc.o + (int64_t)at * kDim + 4 * d);
+    const float to = fmaxf(m, ml.x);
+    const float f = to == -INFINITY ? 1.0f : exp2_fast(m - to), g = to == -INFINITY ? 1.0f : exp2_fast(ml.x - to);
+    o = o * f + x * g;
+    l = l * f + ml.y * g;
+    m = to;
+  }
+  part[slot][d] = o;
+  if (d == 0) part_ml[slot] = float2{m, l};
+  __syncthreads();
+  if (slot > 0) return;
+#pragma unroll
+  for (int i = 1; i < kAtOnce; ++i) {
+    const float2 ml = part_ml[i];
+    const float to = fmaxf(m, ml.x);
+    const float f = to == -INFINITY ? 1.0f : exp2_fast(m - to), g = to == -INFINITY ? 1.0f : exp2_fast(ml.x - to);
+    o = o * f + part[i][d] * g;
+    l = l * f + ml.y * g;
+    m = to;
+  }
+  o *= l > 0.0f ? 1.0f / l : l;
+  const int64_t to = head * a.out_head + cut.x * a.out_request + 4 * d;
+  if constexpr (kType == 0)
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + to) = o;
+  else
+    *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(out) + to) = u32x2{bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};
+  if (lse && d == 0) lse[(int64_t)head * a.requests + cut.x] = (m + __log2f(l)) * kLn2;
 }
 
 template <int kType, int kDim>
 hipError_t launch(const void* q, const void* kp, const void* vp, const uint8_t* ke, const uint8_t* ve, const int32_t* table,
-                  const int32_t* lengths, void* out, float* lse, const DecodeArgs& a, hipStream_t s) {
-  const int64_t groups = (int64_t)a.requests * a.kv_heads * a.qtiles;
-  hipLaunchKernelGGL((paged_attention_kernel<kType, kDim>), dim3((unsigned)groups), dim3(kThreads), 0, s,
+                  const int32_t* lengths, void* out, float* lse, void* workspace, const DecodeArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((paged_attention_kernel<kType, kDim>), dim3(kWaves / (kThreads / 64)), dim3(kThreads), 0, s,
                      static_cast<const char*>(q), static_cast<const char*>(kp), static_cast<const char*>(vp), ke, ve, table,
-                     lengths, static_cast<char*>(out), lse, a);
+                     lengths, static_cast<char*>(out), lse, workspace, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((paged_join_kernel<kType, kDim>), dim3(kWaves, (unsigned)piece_heads(a)), dim3(kThreads), 0, s, workspace,
+                     static_cast<char*>(out), lse, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t paged_attention_workspace(int, const DecodeArgs&) { return 0; }
+int64_t paged_attention_workspace(int dim, const DecodeArgs& a) {
+  return kCutBytes + (int64_t)2 * kWaves * piece_heads(a) * ((int64_t)sizeof(float2) + dim * (int64_t)sizeof(float));
+}
 
 hipError_t launch_paged_attention(int dtype, int dim, const void* q, const void* k_pages,
                                   const void* v_pages, const uint8_t* k_exp, const uint8_t* v_exp,
                                   const int32_t* table, const int32_t* lengths, void* out, float* lse,
-                                  void*, const DecodeArgs& a, hipStream_t s) {
-#define SAF3R_CASE(T, D) \
-  if (dtype == T && dim == D) return launch<T, D>(q, k_pages, v_pages, k_exp, v_exp, table, lengths, out, lse, a, s)
+                                  void* workspace, const DecodeArgs& a, hipStream_t s) {
+#define SAF3R_CASE(T, D)     \
+  if (dtype == T && dim == D) \
+  return launch<T, D>(q, k_pages, v_pages, k_exp, v_exp, table, lengths, out, lse, workspace, a, s)
   SAF3R_CASE(0, 64);
   SAF3R_CASE(0, 128);
   SAF3R_CASE(1, 64);
