@@ -71,6 +71,7 @@ typedef struct {
  *   2. the others, in the order of r, take the pages that they lack for
  *      lengths[r] + new_tokens[r] tokens from the top of the stack, the first
  *      taken being the first that the row lacks.
+ * A page taken or looked up that lies outside [0, pages) gives slots -1.
  * The new tokens of all requests lie one after another, in the order of r:
  * token_start[r] is where those of r start (token_start[requests]: their number;
  * no entry exceeds `tokens`), and slots[t] the cache slot of each, -1 for places
@@ -87,11 +88,13 @@ typedef struct {
  *   free_count                int32 [1]; read as 0 .. pages
  *   page_table                int32 [requests][max_pages]; only the entries of
  *                             the pages taken are written
- *   lengths_out               int32 [requests]; may be `lengths` itself
- *   free_count_out            int32 [1]; may be `free_count` itself
+ *   lengths_out               int32 [requests]; with in_place it may be `lengths`
+ *   free_count_out            int32 [1]; with in_place it may be `free_count`
  *   token_start               int32 [requests + 1]
  *   slots                     int32 [tokens]
- *   workspace                 16-byte aligned, saf3r_page_tables_workspace_bytes
+ *   workspace                 16-byte aligned, saf3r_page_tables_workspace_bytes;
+ *                             may be NULL if these are 0 (up to 1024 requests,
+ *                             with in_place up to 4096 tokens)
  * With separate outputs the call may be repeated: it reads nothing it writes
  * but the pages pushed. All pointers but the workspace 4-byte aligned.
  * Limits: requests 1 .. 65536, max_pages * page_size <= 2^29, tokens 0 .. 2^30. */
@@ -101,6 +104,7 @@ typedef struct {
   int32_t max_pages;  /* entries of a table row, >= 1 */
   int32_t pages;      /* entries of free_pages, >= 1 */
   int32_t tokens;     /* entries of slots */
+  int32_t in_place;   /* 0 or 1 */
 } saf3r_page_step;
 
 /* Bytes of the workspace, or a negative saf3r_status. */
@@ -166,7 +170,8 @@ saf3r_status saf3r_cache_append(const saf3r_page_layout* cache, const saf3r_toke
  *   lengths         int32 [requests]
  *   k_exp, v_exp    of an E4M3 cache (4-byte aligned), else NULL
  *   lse_or_null     NULL, or float32 [q_heads][requests]
- *   workspace       saf3r_paged_attention_workspace_bytes, 16-byte aligned
+ *   workspace       saf3r_paged_attention_workspace_bytes, 16-byte aligned; may be
+ *                   NULL if these are 0
  * Limits: q_heads 1 .. 256 and a multiple of kv_heads, requests 1 .. 65536,
  * max_pages * page_size <= 2^29, anchor >= 0, window >= 0, scale finite and > 0. */
 typedef struct {

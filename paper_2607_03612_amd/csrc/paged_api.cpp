@@ -47,7 +47,9 @@ saf3r_status check_cache(const saf3r_page_layout* c, Cache* out) {
 }
 
 saf3r_status check_step(const saf3r_page_step* p) {
-  if (!p || p->requests <= 0 || p->max_pages <= 0 || p->pages <= 0 || p->tokens < 0) return SAF3R_ERR_INVALID_ARGUMENT;
+  if (!p || p->requests <= 0 || p->max_pages <= 0 || p->pages <= 0 || p->tokens < 0 || p->in_place < 0 ||
+      p->in_place > 1)
+    return SAF3R_ERR_INVALID_ARGUMENT;
   const saf3r_status st = check_page_size(p->page_size);
   if (st != SAF3R_OK) return st;
   if (p->requests > saf3r::kMaxRequests || (int64_t)p->max_pages * p->page_size > saf3r::kMaxRowTokens ||
@@ -103,6 +105,7 @@ extern "C" {
 int64_t saf3r_page_tables_workspace_bytes(const saf3r_page_step* step) {
   const saf3r_status st = check_step(step);
   if (st != SAF3R_OK) return st;
+  if (saf3r::page_tables_in_one(step->requests, step->tokens, step->in_place != 0)) return 0;
   return (int64_t)step->requests * (int64_t)sizeof(saf3r::RequestRecord);
 }
 
@@ -117,14 +120,18 @@ saf3r_status saf3r_page_tables(const saf3r_page_step* step, const int32_t* lengt
   const void* words[] = {lengths, new_tokens, free_pages, free_count, page_table, lengths_out, free_count_out, token_start};
   for (const void* p : words)
     if (!p || !aligned(p, 4)) return SAF3R_ERR_INVALID_ARGUMENT;
-  if ((step->tokens > 0 && !slots) || !aligned(slots, 4) || !workspace || !aligned(workspace, 16) || workspace_bytes < 0)
+  if (!step->in_place && (lengths_out == lengths || free_count_out == free_count)) return SAF3R_ERR_INVALID_ARGUMENT;
+  const int64_t need = saf3r_page_tables_workspace_bytes(step);
+  if ((step->tokens > 0 && !slots) || !aligned(slots, 4) || (need > 0 && !workspace) || !aligned(workspace, 16) ||
+      workspace_bytes < 0)
     return SAF3R_ERR_INVALID_ARGUMENT;
-  if (workspace_bytes < saf3r_page_tables_workspace_bytes(step)) return SAF3R_ERR_CAPACITY;
+  if (workspace_bytes < need) return SAF3R_ERR_CAPACITY;
   saf3r::StepArgs a{};
   a.requests = step->requests;
   a.max_pages = step->max_pages;
   a.pages = step->pages;
   a.tokens = step->tokens;
+  a.in_place = step->in_place;
   a.page = saf3r::page_div(step->page_size);
   return hip_status(saf3r::launch_page_tables(lengths, new_tokens, free_pages, free_count, page_table, lengths_out,
                                               free_count_out, token_start, slots,
@@ -165,7 +172,7 @@ int64_t saf3r_paged_attention_workspace_bytes(const saf3r_page_layout* cache, co
   saf3r::DecodeArgs a{};
   const saf3r_status st = check_decode(cache, step, &c, &a);
   if (st != SAF3R_OK) return st;
-  return saf3r::paged_attention_workspace(cache->head_dim, a);
+  return saf3r::paged_attention_workspace(cache->dtype, cache->head_dim, a);
 }
 
 saf3r_status saf3r_paged_attention(const saf3r_page_layout* cache, const saf3r_decode* step,
@@ -178,13 +185,15 @@ saf3r_status saf3r_paged_attention(const saf3r_page_layout* cache, const saf3r_d
   saf3r::DecodeArgs a{};
   const saf3r_status st = check_decode(cache, step, &c, &a);
   if (st != SAF3R_OK) return st;
-  const void* wide[] = {q, k_pages, v_pages, out, workspace};
+  const void* wide[] = {q, k_pages, v_pages, out};
   for (const void* p : wide)
     if (!p || !aligned(p, 16)) return SAF3R_ERR_INVALID_ARGUMENT;
+  const int64_t need = saf3r::paged_attention_workspace(cache->dtype, cache->head_dim, a);
+  if ((need > 0 && !workspace) || !aligned(workspace, 16)) return SAF3R_ERR_INVALID_ARGUMENT;
   if (!page_table || !lengths || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(lse_or_null, 4) ||
       !exps_ok(cache->dtype, k_exp, v_exp) || workspace_bytes < 0)
     return SAF3R_ERR_INVALID_ARGUMENT;
-  if (workspace_bytes < saf3r::paged_attention_workspace(cache->head_dim, a)) return SAF3R_ERR_CAPACITY;
+  if (workspace_bytes < need) return SAF3R_ERR_CAPACITY;
   return hip_status(saf3r::launch_paged_attention(cache->dtype, cache->head_dim, q, k_pages, v_pages, k_exp, v_exp,
                                                   page_table, lengths, out, lse_or_null, workspace, a,
                                                   static_cast<hipStream_t>(stream)));

@@ -22,12 +22,17 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+// Shared-out launches: 512 workgroups of four waves, two waves to a SIMD. Each wave
+// takes the same number of tiles, at least kMinTiles, so that a short launch does
+// not spend itself on joining.
 constexpr int kThreads = 256;
-constexpr int kCuCount = 256;
-// Waves of a launch, two to a SIMD: every wave takes the same number of tiles, at
-// least kMinTiles, so that a short launch does not spend itself on joining.
-constexpr int kWaves = kCuCount * 8;
+constexpr int kGroupWaves = kThreads / 64;
+constexpr int kWorkgroups = 512;
+constexpr int kWaves = kWorkgroups * kGroupWaves;  // a power of two
 constexpr int kMinTiles = 2;
+// Whole-row launches: eight waves share a row.
+constexpr int kRowThreads = 512;
+constexpr int kRowWaves = kRowThreads / 64;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // kType: 0 fp32, 1 bf16, 2 e4m3.
@@ -35,7 +40,8 @@ template <int kType, int kDim>
 struct Shape {
   static constexpr int kSize = kType == 0 ? 4 : kType == 1 ? 2 : 1;  // bytes of a cached value
   static constexpr int kVDims = kDim / 16;                           // dimensions of V per lane
-  // 16-key groups of a tile: 32 to 64 registers of K and V in flight per lane
+  // 16-key groups of a tile: 32 to 64 registers of K and V in flight per lane (four for
+  // bf16 of 64 as well: 16.7 -> 21.7 us for 1024 rows of 512 tokens)
   static constexpr int kGroups = kType == 0 ? (kDim == 64 ? 2 : 1) : kType == 1 ? 2 : 4;
   static constexpr int kTile = 16 * kGroups;            // keys
   static constexpr int kKWords = kDim * kSize / 16;     // words of K per lane and group
@@ -63,13 +69,20 @@ struct State {
 };
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// Over the four lanes of a query: lanes 32 and 16 apart, exchanged in registers.
 __device__ inline float across_groups_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  const uint32_t w = __float_as_uint(x);
+  const auto s = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  const uint32_t y = __float_as_uint(fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])));
+  const auto t = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+  return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
 }
 __device__ inline float across_groups_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  const uint32_t w = __float_as_uint(x);
+  const auto s = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  const uint32_t y = __float_as_uint(__uint_as_float(s[0]) + __uint_as_float(s[1]));
+  const auto t = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 
 // Tokens of a request that are attended, in tiles: the first `head` tiles, and
@@ -103,35 +116,86 @@ __device__ inline Span span_of(const DecodeArgs& a, int32_t length) {
   return s;
 }
 
-// One tile of a request's row: what it is and where its keys lie.
+// One tile of a row: what it is and where its keys lie. A row is a request's
+// key-value head h with up to 16 of the query heads that share it.
 template <int kGroups>
 struct Place {
-  int32_t r;     // request
-  int32_t row;   // of its rows (key-value head, tile of query heads)
-  int32_t x;     // tile of the row, of s.count
-  int32_t tile;  // the same counted from the sequence's start
+  int32_t r;             // request
+  int32_t h, qt;         // key-value head, tile of its query heads
+  int32_t first, heads;  // query heads first .. first + heads - 1
+  int32_t x;             // tile of the row, of s.count
+  int32_t tile;          // the same counted from the sequence's start
   Span s;
-  int32_t page[kGroups];  // -1 for a page that holds no token or whose entry is no page
-  int64_t at[kGroups];    // bytes from a head's pages to the group's first key
-  int64_t exp[kGroups];   // entries to its exponents
+  uint32_t absent;       // bit u: group u's page holds no token, or its entry is no page
+  int64_t head, exp_head;  // bytes to the head in a page, entries to its exponents
+  int64_t at[kGroups];   // bytes to the group's first key
+  int64_t exp[kGroups];  // entries to its exponents
+  __device__ void set_row(const DecodeArgs& a) {
+    first = h * a.group + 16 * qt;
+    heads = min(a.group - 16 * qt, 16);
+    head = h * a.head_stride;
+    exp_head = (int64_t)h * a.page.size;
+  }
+  // the next row of the request; false if that was its last
+  __device__ bool next_row(const DecodeArgs& a) {
+    x = 0;
+    bool more = true;
+    if (++qt == a.qtiles) {
+      qt = 0;
+      if (++h == a.kv_heads) {
+        h = 0;
+        more = false;
+      }
+    }
+    set_row(a);
+    return more;
+  }
 };
 
-template <int kGroups>
-__device__ inline void look_up(const DecodeArgs& a, const int32_t* __restrict__ table, Place<kGroups>& p) {
+// 64 entries of a request's row of the table, one a lane: a tile's pages come from
+// there without a trip to memory.
+struct Entries {
+  int32_t r, base;
+  int32_t page;  // entry base + lane; -1 past the request's pages and for what is no page
+};
+
+template <int kType, int kGroups>
+__device__ inline void look_up(const DecodeArgs& a, const int32_t* __restrict__ table, Entries& e, Place<kGroups>& p) {
   p.tile = p.x < p.s.head ? p.x : p.x + p.s.skip;
-  const int h = p.row / a.qtiles;
+  p.absent = 0;
+  const int32_t pos = p.tile * (16 * kGroups);
+  int32_t i = div_page(a.page, pos), in = pos - i * a.page.size;
 #pragma unroll
   for (int u = 0; u < kGroups; ++u) {
-    const int32_t pos = p.tile * (16 * kGroups) + 16 * u;
-    const int32_t i = div_page(a.page, pos);
-    int32_t page = pos < p.s.n ? table[(int64_t)p.r * a.max_pages + i] : -1;
-    page = page < 0 || page >= a.pages ? -1 : page;
-    // an absent page's keys are read from page 0, which exists, and masked
-    const int32_t in = page < 0 ? 0 : pos - i * a.page.size;
-    const int64_t from = max(page, 0);
-    p.page[u] = page;
-    p.at[u] = from * a.page_stride + h * a.head_stride + (int64_t)in * a.token_stride;
-    p.exp[u] = (from * a.kv_heads + h) * a.page.size + in;
+    if (u > 0) {
+      in += 16;
+      if (in == a.page.size) {
+        in = 0;
+        ++i;
+      }
+    }
+    if (u == 0 || in == 0) {
+      if (p.r != e.r || (uint32_t)(i - e.base) >= 64u) {
+        e.r = p.r;
+        e.base = i;
+        const int32_t j = i + (threadIdx.x & 63);
+        e.page = j * a.page.size < p.s.n ? table[(int64_t)p.r * a.max_pages + j] : -1;
+        e.page = (uint32_t)e.page < (uint32_t)a.pages ? e.page : -1;
+        // waited for here: left to its first use, the wait would be one for every
+        // load in flight on every tile
+        asm volatile("" : "+v"(e.page));
+      }
+      // an absent page's keys are read from page 0, which exists, and masked
+      const int32_t page = __builtin_amdgcn_readlane(e.page, i - e.base);
+      p.absent |= (uint32_t)(page < 0) << u;
+      const uint32_t from = (uint32_t)max(page, 0);
+      p.at[u] = p.head + from * a.page_stride + (int64_t)in * a.token_stride;
+      if constexpr (kType == 2) p.exp[u] = p.exp_head + from * (int64_t)(a.kv_heads * a.page.size) + in;
+    } else {
+      p.absent |= (p.absent >> (u - 1) & 1u) << u;
+      p.at[u] = p.at[u - 1] + 16 * a.token_stride;
+      if constexpr (kType == 2) p.exp[u] = p.exp[u - 1] + 16;
+    }
   }
 }
 
@@ -196,7 +260,9 @@ __device__ inline uint32_t fp8_pair(uint32_t codes, bool high, float scale) {
 }
 // Two fp32 as bf16 (nearest, ties to even), the first in the low half.
 __device__ inline uint32_t bf16_pair(float x, float y) {
-  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
+  uint32_t r;
+  asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
+  return r;
 }
 
 // S^T of a tile.
@@ -236,10 +302,7 @@ __device__ inline void score_tile(const KeyTile<kType, kDim>& t, const uint32_t 
 template <int kGroups>
 __device__ inline bool is_whole(const Place<kGroups>& p) {
   const int32_t first = p.tile * (16 * kGroups), last = first + 16 * kGroups;
-  bool whole = last <= p.s.n && (last <= p.s.anchor || first >= p.s.from);
-#pragma unroll
-  for (int u = 0; u < kGroups; ++u) whole = whole && p.page[u] >= 0;
-  return whole;
+  return p.absent == 0 && last <= p.s.n && (last <= p.s.anchor || first >= p.s.from);
 }
 
 // A tile's scores and V into the running softmax. With scores z in log2 units and
@@ -256,7 +319,7 @@ __device__ inline void add_tile(const DecodeArgs& a, const Place<Shape<kType, kD
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int32_t j = first + 16 * u + 4 * g + r;
-        const bool keep = pl.page[u] >= 0 && j < pl.s.n && (j < pl.s.anchor || j >= pl.s.from);
+        const bool keep = !(pl.absent >> u & 1u) && j < pl.s.n && (j < pl.s.anchor || j >= pl.s.from);
         if (!keep) {
           z[u][r] = -INFINITY;
 #pragma unroll
@@ -338,17 +401,15 @@ __device__ inline void add_tile(const DecodeArgs& a, const Place<Shape<kType, kD
 // The queries of a tile of 16 heads: lane % 16 is the query, the pieces of its
 // row those of K's rows. Heads past the group are zeros.
 template <int kType, int kDim>
-__device__ inline void load_queries(const DecodeArgs& a, const char* __restrict__ q, int r, int row,
-                                    uint32_t (&w)[Shape<kType, kDim>::kQWords]) {
+__device__ inline void load_queries(const DecodeArgs& a, const char* __restrict__ q,
+                                    const Place<Shape<kType, kDim>::kGroups>& p, uint32_t (&w)[Shape<kType, kDim>::kQWords]) {
   using S = Shape<kType, kDim>;
-  const int qt = row % a.qtiles, first = row / a.qtiles * a.group + 16 * qt;
-  const int heads = min(a.group - 16 * qt, 16);
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   constexpr int kIn = kType == 0 ? 4 : 2;
 #pragma unroll
   for (int x = 0; x < S::kQWords; ++x) w[x] = 0;
-  if (c < heads) {
-    const char* row = q + ((first + c) * a.q_head + r * a.q_request) * kIn;
+  if (c < p.heads) {
+    const char* row = q + ((p.first + c) * a.q_head + p.r * a.q_request) * kIn;
     if constexpr (kType == 2) {
       // K's piece of 16 codes is two products' share: 32 bytes of q
 #pragma unroll
@@ -363,167 +424,128 @@ __device__ inline void load_queries(const DecodeArgs& a, const char* __restrict_
   }
 }
 
-// Where a launch's pieces go: a row that falls to several waves leaves a part in
-// each, wave w's in slot 2w if the row began before the wave's tiles and in slot
-// 2w + 1 if it begins among them. Each part: kDim sums per query, and (m, l).
-struct Pieces {
-  float* o;    // [2 kWaves][heads][kDim]
-  float2* ml;  // [2 kWaves][heads]
-  int4* cut;   // a row that starts in wave w and ends in a later one: (request, row, w, last wave), else w < 0
+// Parts of rows in LDS: of each its sums and (m, l) per query.
+constexpr int kSlots = 8;
+template <int kDim>
+struct Parts {
+  float o[kSlots][16][kDim + 4];
+  float2 ml[kSlots][16];
 };
-constexpr int64_t kCutBytes = (int64_t)kWaves * sizeof(int4);
 
-__host__ __device__ inline Pieces pieces(void* workspace, int heads) {
-  Pieces p;
-  p.cut = static_cast<int4*>(workspace);
-  p.ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + kCutBytes);
-  p.o = reinterpret_cast<float*>(p.ml + 2 * kWaves * heads);
-  return p;
-}
-__host__ __device__ inline int piece_heads(const DecodeArgs& a) { return a.group < 16 ? a.group : 16; }
-
-// A wave's part of a row: the output where it has the whole row, else a piece.
 template <int kType, int kDim>
-__device__ inline void put_row(const DecodeArgs& a, const State<kType, kDim>& st, int r, int row, int slot, char* __restrict__ out,
-                               float* __restrict__ lse, const Pieces& pc) {
+__device__ inline void put_part(Parts<kDim>& lds, int slot, const State<kType, kDim>& st) {
   using S = Shape<kType, kDim>;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
-  const int qt = row % a.qtiles, first = row / a.qtiles * a.group + 16 * qt;
-  const int heads = min(a.group - 16 * qt, 16);
   const float l = across_groups_sum(st.l);
-  if (c >= heads) return;
-  if (slot >= 0) {
-    const int at = slot * piece_heads(a) + c;
-    if (g == 0) pc.ml[at] = float2{st.m, l};
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int i = 0; i < S::kVDims; i += 4)
-        *reinterpret_cast<f32x4*>(pc.o + (int64_t)at * kDim + (4 * g + x) * S::kVDims + i) =
-            f32x4{st.o[i][x], st.o[i + 1][x], st.o[i + 2][x], st.o[i + 3][x]};
-    return;
-  }
-  const float f = l > 0.0f ? 1.0f / l : l;  // 0 and NaN stay
-  const int head = first + c;
-  const int64_t at = head * a.out_head + r * a.out_request;
+  if (g == 0) lds.ml[slot][c] = float2{st.m, l};
 #pragma unroll
   for (int x = 0; x < 4; ++x)
 #pragma unroll
-    for (int i = 0; i < S::kVDims; i += 4) {
-      const int64_t to = at + (4 * g + x) * S::kVDims + i;
-      const f32x4 y = f32x4{st.o[i][x], st.o[i + 1][x], st.o[i + 2][x], st.o[i + 3][x]} * f;
-      if constexpr (kType == 0)
-        *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + to) = y;
-      else
-        *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(out) + to) = u32x2{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])};
-    }
-  if (lse && g == 0) lse[(int64_t)head * a.requests + r] = (st.m + __log2f(l)) * kLn2;
+    for (int i = 0; i < S::kVDims; i += 4)
+      *reinterpret_cast<f32x4*>(&lds.o[slot][c][(4 * g + x) * S::kVDims + i]) =
+          f32x4{st.o[i][x], st.o[i + 1][x], st.o[i + 2][x], st.o[i + 3][x]};
 }
 
-// The next request after r that has tiles (64 lengths at a time), or `requests`.
-template <int kTile>
-__device__ inline int next_request(const DecodeArgs& a, const int32_t* __restrict__ lengths, int r) {
-  const int lane = threadIdx.x & 63;
-  for (++r; r < a.requests; r += 64) {
-    const bool some = r + lane < a.requests && lengths[r + lane] > 0;
-    const uint64_t found = __ballot(some);
-    if (found) return r + __ffsll((unsigned long long)found) - 1;
+// kWidth neighbouring sums of a query, and its (m, l).
+template <int kWidth>
+struct Sums {
+  float o[kWidth];
+  float m, l;
+  __device__ void clear() {
+    m = -INFINITY;
+    l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kWidth; ++i) o[i] = 0.0f;
   }
-  return a.requests;
+  __device__ void add(const float* x, float2 ml) {
+    const float to = fmaxf(m, ml.x);
+    const float f = to == -INFINITY ? 1.0f : exp2_fast(m - to), g = to == -INFINITY ? 1.0f : exp2_fast(ml.x - to);
+#pragma unroll
+    for (int i = 0; i < kWidth; ++i) o[i] = fmaf(x[i], g, o[i] * f);
+    l = fmaf(ml.y, g, l * f);
+    m = to;
+  }
+};
+
+template <int kType, int kWidth>
+__device__ inline void put_values(const DecodeArgs& a, char* __restrict__ out, int r, int head, int d, const float* x) {
+  const int64_t at = head * a.out_head + r * a.out_request + d;
+  if constexpr (kType == 0) {
+#pragma unroll
+    for (int i = 0; i < kWidth; i += 2) {
+      float* to = reinterpret_cast<float*>(out) + at + i;
+      if constexpr (kWidth % 4 == 0) {
+        if (i % 4 == 0) *reinterpret_cast<f32x4*>(to) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+      } else {
+        *reinterpret_cast<float2*>(to) = float2{x[i], x[i + 1]};
+      }
+    }
+  } else {
+    uint32_t w[kWidth / 2];
+#pragma unroll
+    for (int i = 0; i < kWidth / 2; ++i) w[i] = bf16_pair(x[2 * i], x[2 * i + 1]);
+    uint16_t* to = reinterpret_cast<uint16_t*>(out) + at;
+    if constexpr (kWidth == 8)
+      *reinterpret_cast<u32x4*>(to) = u32x4{w[0], w[1], w[2], w[3]};
+    else if constexpr (kWidth == 4)
+      *reinterpret_cast<u32x2*>(to) = u32x2{w[0], w[1]};
+    else
+      *reinterpret_cast<uint32_t*>(to) = w[0];
+  }
 }
 
-// The tiles of all requests' rows, request by request and row by row, are dealt
-// out to the waves in equal runs of neighbouring tiles. A wave goes through its
-// run without a stop: while it works on one tile's scores the next one's K is on
-// the way, while it works on V the next V.
+// The finished output of kWidth dimensions; a query without a key has l = 0.
+template <int kType, int kWidth>
+__device__ inline void put_output(const DecodeArgs& a, char* __restrict__ out, float* __restrict__ lse, int r, int head, int d,
+                                  const float* o, float m, float l) {
+  const float f = l > 0.0f ? 1.0f / l : l;  // 0 and NaN stay
+  float x[kWidth];
+#pragma unroll
+  for (int i = 0; i < kWidth; ++i) x[i] = o[i] * f;
+  put_values<kType, kWidth>(a, out, r, head, d, x);
+  if (lse && d == 0) lse[(int64_t)head * a.requests + r] = (m + __log2f(l)) * kLn2;
+}
+
+// A row that one wave has whole.
 template <int kType, int kDim>
-__global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
-    const char* __restrict__ q, const char* __restrict__ k, const char* __restrict__ v,
-    const uint8_t* __restrict__ k_exp, const uint8_t* __restrict__ v_exp, const int32_t* __restrict__ table,
-    const int32_t* __restrict__ lengths, char* __restrict__ out, float* __restrict__ lse, void* __restrict__ workspace,
-    DecodeArgs a) {
+__device__ inline void put_row(const DecodeArgs& a, const State<kType, kDim>& st,
+                               const Place<Shape<kType, kDim>::kGroups>& p, char* __restrict__ out, float* __restrict__ lse) {
   using S = Shape<kType, kDim>;
-  __shared__ int64_t before[kThreads + 1];  // tiles of the requests before a thread's
-  __shared__ int64_t wave_sum[kThreads / 64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = a.kv_heads * a.qtiles;
-  const Pieces pc = pieces(workspace, piece_heads(a));
-
-  // requests without a token
-  for (int r = blockIdx.x; r < a.requests; r += gridDim.x) {
-    if (lengths[r] > 0) continue;
-    for (int i = threadIdx.x; i < a.q_heads * (kDim / 4); i += kThreads) {
-      const int head = i / (kDim / 4), d = i % (kDim / 4) * 4;
-      const int64_t at = head * a.out_head + r * a.out_request + d;
-      if constexpr (kType == 0)
-        *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + at) = f32x4{0, 0, 0, 0};
-      else
-        *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(out) + at) = u32x2{0, 0};
-      if (lse && d == 0) lse[(int64_t)head * a.requests + r] = -INFINITY;
-    }
-  }
-
-  // where the runs lie: each thread counts neighbouring requests
-  const int each = (a.requests + kThreads - 1) / kThreads;
-  int64_t mine = 0;
-  for (int i = 0; i < each; ++i) {
-    const int r = threadIdx.x * each + i;
-    if (r < a.requests) mine += span_of<S::kTile>(a, lengths[r]).count;
-  }
-  mine *= rows;
-  int64_t sum = mine;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const float l = across_groups_sum(st.l);
+  if (c >= p.heads) return;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up(sum, d);
-    if (lane >= d) sum += y;
-  }
-  if (lane == 63) wave_sum[wave] = sum;
-  __syncthreads();
-  int64_t total = 0;
+  for (int x = 0; x < 4; ++x) {
+    float o[S::kVDims];
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    if (w == wave) sum += total;
-    total += wave_sum[w];
+    for (int i = 0; i < S::kVDims; ++i) o[i] = st.o[i][x];
+    put_output<kType, S::kVDims>(a, out, lse, p.r, p.first + c, (4 * g + x) * S::kVDims, o, st.m, l);
   }
-  before[threadIdx.x] = sum - mine;
-  __syncthreads();
+}
 
-  const int64_t run = max((total + kWaves - 1) / kWaves, (int64_t)kMinTiles);
-  const int w = wave * gridDim.x + blockIdx.x;  // neighbouring runs on different CUs
-  const int64_t lo = w * run, hi = min(lo + run, total);
-  if (lane == 0) pc.cut[w].z = -1;
-  if (lo >= hi) return;
-
-  // the first tile's request: the thread whose requests hold it, then these one by one
-  int owner = 0;
-#pragma unroll
-  for (int i = 0; i < kThreads / 64; ++i) owner += __popcll(__ballot(before[64 * i + lane] <= lo));
-  owner -= 1;
-  Place<S::kGroups> next;
-  next.r = owner * each;
-  int64_t off = lo - before[owner];
-  next.s = span_of<S::kTile>(a, lengths[next.r]);
-  while (off >= (int64_t)next.s.count * rows) {
-    off -= (int64_t)next.s.count * rows;
-    next.s = span_of<S::kTile>(a, lengths[++next.r]);
-  }
-  next.r = __builtin_amdgcn_readfirstlane(next.r);
-  next.s = span_of<S::kTile>(a, lengths[next.r]);
-  next.row = (int32_t)(off / next.s.count);
-  next.row = __builtin_amdgcn_readfirstlane(next.row);
-  next.x = __builtin_amdgcn_readfirstlane((int32_t)(off - (int64_t)next.row * next.s.count));
-
+// A wave goes through `left` > 0 tiles from `next` on without a stop: the next tile's
+// K is asked for as soon as the present scores are there, its V behind the present
+// sums. advance(next) goes to the following tile and says whether it begins another
+// row; done(state, place, from_start, ends) takes the part of a row. (Both asked for
+// a whole tile ahead, in registers of their own: no faster anywhere, 16.7 / 20.7 us
+// for 1024 rows of 512 tokens. One CU takes in 40 to 60 bytes a ns either way.)
+template <int kType, int kDim, typename Advance, typename Done>
+__device__ inline void walk(const DecodeArgs& a, const char* __restrict__ q, const char* __restrict__ k,
+                            const char* __restrict__ v, const uint8_t* __restrict__ k_exp, const uint8_t* __restrict__ v_exp,
+                            const int32_t* __restrict__ table, Place<Shape<kType, kDim>::kGroups>& next, int64_t left,
+                            Advance advance, Done done) {
+  using S = Shape<kType, kDim>;
   KeyTile<kType, kDim> kt;
   ValueTile<kType, kDim> vt;
   State<kType, kDim> st;
   uint32_t qw[S::kQWords], qn[S::kQWords];
-  look_up<S::kGroups>(a, table, next);
-  load_queries<kType, kDim>(a, q, next.r, next.row, qn);
+  Entries entries{-1, 0, -1};
+  load_queries<kType, kDim>(a, q, next, qn);
+  look_up<kType>(a, table, entries, next);
   load_keys<kType, kDim>(a, k, k_exp, next, kt);
   load_values<kType, kDim>(a, v, v_exp, next, vt);
-  bool begins = true;         // the tile is the wave's first of its row
-  bool from_start = next.x == 0;  // and the row's first
-  int64_t left = hi - lo;
+  bool begins = true;      // the tile is the wave's first of its row
+  bool from_start = true;  // and that the row's first
   while (true) {
     const Place<S::kGroups> now = next;
     if (begins) {
@@ -538,106 +560,339 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
     f32x4 z[S::kGroups];
     score_tile<kType, kDim>(kt, qw, z);
     const bool ends = now.x + 1 == now.s.count;
-    --left;
-    if (left > 0) {
-      if (!ends) {
-        ++next.x;
-      } else {
-        next.x = 0;
-        if (++next.row == rows) {
-          next.row = 0;
-          next.r = __builtin_amdgcn_readfirstlane(next_request<S::kTile>(a, lengths, next.r));
-          next.s = span_of<S::kTile>(a, lengths[next.r]);
-        }
-        load_queries<kType, kDim>(a, q, next.r, next.row, qn);
-      }
-      look_up<S::kGroups>(a, table, next);
+    const bool last = --left == 0;
+    if (!last) {
+      if (advance(next)) load_queries<kType, kDim>(a, q, next, qn);
+      look_up<kType>(a, table, entries, next);
       load_keys<kType, kDim>(a, k, k_exp, next, kt);
     }
     add_tile<kType, kDim>(a, now, z, vt, st);
-    if (left > 0) load_values<kType, kDim>(a, v, v_exp, next, vt);
+    if (!last) load_values<kType, kDim>(a, v, v_exp, next, vt);
     begins = ends;
-    if (ends || left == 0) {
-      const bool whole = ends && from_start;
-      put_row<kType, kDim>(a, st, now.r, now.row, whole ? -1 : from_start ? 2 * w + 1 : 2 * w, out, lse, pc);
-      if (!ends && from_start && lane == 0) {
-        // tiles of the row behind this run, a run each wave
-        const int64_t behind = now.s.count - 1 - now.x;
-        pc.cut[w] = int4{now.r, now.row, w, w + (int)((behind + run - 1) / run)};
-      }
-    }
-    if (left == 0) break;
+    if (ends || last) done(st, now, from_start, ends);
+    if (last) break;
   }
 }
 
-// The rows that fell to several waves: one workgroup per such row and query, its
-// 16-byte lanes spread over kThreads * 4 / kDim pieces at a time, in the order of
-// the waves.
+// ------------------------------------------------- rows shared out among all
+
+// Where a launch's pieces go: a row that falls to several workgroups leaves a part
+// in each, workgroup w's in slot 2w if the row began before it and in slot 2w + 1 if
+// it begins there. Each part: kDim sums per query, and (m, l).
+struct Pieces {
+  float* o;    // [2 kWorkgroups][heads][kDim]
+  float2* ml;  // [2 kWorkgroups][heads]
+  int4* cut;   // a row that begins in workgroup w and ends in a later one: (request, first query head and, from
+               // bit 16 on, their number, w, last one), else z < 0
+};
+constexpr int64_t kCutBytes = (int64_t)kWorkgroups * sizeof(int4);
+
+__host__ __device__ inline Pieces pieces(void* workspace, int heads) {
+  Pieces p;
+  p.cut = static_cast<int4*>(workspace);
+  p.ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + kCutBytes);
+  p.o = reinterpret_cast<float*>(p.ml + 2 * kWorkgroups * heads);
+  return p;
+}
+__host__ __device__ inline int piece_heads(const DecodeArgs& a) { return a.group < 16 ? a.group : 16; }
+
+// The next request after r that has tiles (64 lengths at a time), or `requests`.
+__device__ inline int next_request(const DecodeArgs& a, const int32_t* __restrict__ lengths, int r) {
+  const int lane = threadIdx.x & 63;
+  for (++r; r < a.requests; r += 64) {
+    const bool some = r + lane < a.requests && lengths[r + lane] > 0;
+    const uint64_t found = __ballot(some);
+    if (found) return __builtin_amdgcn_readfirstlane(r + __ffsll((unsigned long long)found) - 1);
+  }
+  return a.requests;
+}
+
+// The first tile of a wave's run.
+__device__ inline int64_t run_start(int64_t total, int wave) {
+  return total < (int64_t)kWaves * kMinTiles ? min((int64_t)wave * kMinTiles, total) : total * wave / kWaves;
+}
+// The wave whose run holds tile x.
+__device__ inline int run_of(int64_t total, int64_t x) {
+  return total < (int64_t)kWaves * kMinTiles ? (int)(x / kMinTiles) : (int)(((x + 1) * kWaves - 1) / total);
+}
+
+// The outputs of requests without a token, every kWorkgroups-th request.
+template <int kType, int kDim>
+__device__ inline void zero_rows(const DecodeArgs& a, const int32_t* __restrict__ lengths, char* __restrict__ out,
+                                 float* __restrict__ lse, int w) {
+  for (int r = w; r < a.requests; r += kWorkgroups) {
+    if (lengths[r] > 0) continue;
+    for (int i = threadIdx.x; i < a.q_heads * (kDim / 4); i += kThreads) {
+      const float none[4] = {0, 0, 0, 0};
+      put_output<kType, 4>(a, out, lse, r, i / (kDim / 4), i % (kDim / 4) * 4, none, -INFINITY, 0.0f);
+    }
+  }
+}
+
+struct PartHead {
+  int32_t r;
+  int32_t first, heads;
+  int32_t ends;    // 1: the row's last tile is in it; 0: not; -1: no part
+  int32_t behind;  // tiles of the row behind it
+};
+
+// The tiles of all requests' rows, request by request and row by row, are dealt out
+// to the waves in equal runs of neighbouring tiles.
+template <int kType, int kDim>
+__global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
+    const char* __restrict__ q, const char* __restrict__ k, const char* __restrict__ v,
+    const uint8_t* __restrict__ k_exp, const uint8_t* __restrict__ v_exp, const int32_t* __restrict__ table,
+    const int32_t* __restrict__ lengths, char* __restrict__ out, float* __restrict__ lse, void* __restrict__ workspace,
+    DecodeArgs a) {
+  using S = Shape<kType, kDim>;
+  __shared__ union {
+    struct {
+      int64_t before[kThreads];  // tiles of the requests before a thread's
+      int64_t wave_sum[kGroupWaves];
+      int32_t length[kThreads];  // of a thread's first request
+    } deal;
+    Parts<kDim> parts;
+  } lds;
+  __shared__ PartHead heads_of[kSlots];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = a.kv_heads * a.qtiles;
+  const int w = blockIdx.x;
+  const Pieces pc = pieces(workspace, piece_heads(a));
+
+  // where the runs lie: each thread counts neighbouring requests
+  const int each = (a.requests + kThreads - 1) / kThreads;
+  int64_t mine = 0;
+  for (int i = 0; i < each; ++i) {
+    const int r = threadIdx.x * each + i;
+    const int32_t length = r < a.requests ? lengths[r] : 0;
+    if (i == 0) lds.deal.length[threadIdx.x] = length;
+    mine += span_of<S::kTile>(a, length).count;
+  }
+  mine *= rows;
+  int64_t sum = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(sum, d);
+    if (lane >= d) sum += y;
+  }
+  if (lane == 63) lds.deal.wave_sum[wave] = sum;
+  if (threadIdx.x < kSlots) heads_of[threadIdx.x].ends = -1;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int i = 0; i < kGroupWaves; ++i) {
+    if (i == wave) sum += total;
+    total += lds.deal.wave_sum[i];
+  }
+  lds.deal.before[threadIdx.x] = sum - mine;
+  __syncthreads();
+
+  if (threadIdx.x == 0) pc.cut[w].z = -1;
+  if (run_start(total, w * kGroupWaves) >= total) {  // the whole workgroup
+    zero_rows<kType, kDim>(a, lengths, out, lse, w);
+    return;
+  }
+  const int64_t lo = run_start(total, w * kGroupWaves + wave), hi = run_start(total, w * kGroupWaves + wave + 1);
+
+  Place<S::kGroups> next;
+  if (lo < hi) {
+    // the first tile's request: the thread whose requests hold it, then these one by one
+    int owner = -1;
+#pragma unroll
+    for (int i = 0; i < kGroupWaves; ++i) owner += __popcll(__ballot(lds.deal.before[64 * i + lane] <= lo));
+    int64_t off = lo - lds.deal.before[owner];
+    next.r = __builtin_amdgcn_readfirstlane(owner * each);
+    next.s = span_of<S::kTile>(a, __builtin_amdgcn_readfirstlane(lds.deal.length[owner]));
+    while (off >= (int64_t)next.s.count * rows) {
+      off -= (int64_t)next.s.count * rows;
+      next.s = span_of<S::kTile>(a, lengths[++next.r]);
+    }
+    const int32_t row = __builtin_amdgcn_readfirstlane((int32_t)(off / next.s.count));
+    next.x = __builtin_amdgcn_readfirstlane((int32_t)(off - (int64_t)row * next.s.count));
+    next.h = row / a.qtiles;
+    next.qt = row - next.h * a.qtiles;
+    next.set_row(a);
+  }
+  __syncthreads();  // the parts go where the counts were
+  if (lo < hi) {
+    walk<kType, kDim>(
+        a, q, k, v, k_exp, v_exp, table, next, hi - lo,
+        [&](Place<S::kGroups>& p) {
+          if (++p.x < p.s.count) return false;
+          if (!p.next_row(a)) {
+            p.r = next_request(a, lengths, p.r);
+            p.s = span_of<S::kTile>(a, lengths[p.r]);
+          }
+          return true;
+        },
+        [&](const State<kType, kDim>& st, const Place<S::kGroups>& p, bool from_start, bool ends) {
+          if (from_start && ends) {
+            put_row<kType, kDim>(a, st, p, out, lse);
+          } else {
+            const int slot = 2 * wave + (from_start ? 1 : 0);
+            put_part<kType, kDim>(lds.parts, slot, st);
+            if (lane == 0) heads_of[slot] = PartHead{p.r, p.first, p.heads, ends ? 1 : 0, p.s.count - 1 - p.x};
+          }
+        });
+  }
+  __syncthreads();
+
+  // the parts in their order: those of one row follow one another
+  constexpr int kWidth = kDim * 16 / kThreads;
+  const int c = threadIdx.x >> 4, d = (threadIdx.x & 15) * kWidth;
+  Sums<kWidth> sums;
+  bool open = false, begun = false;
+  for (int slot = 0; slot < kSlots; ++slot) {
+    const PartHead h = heads_of[slot];
+    if (h.ends < 0) continue;
+    if (!open) {
+      sums.clear();
+      begun = (slot & 1) != 0;
+      open = true;
+    }
+    sums.add(&lds.parts.o[slot][c][d], lds.parts.ml[slot][c]);
+    bool more = false;  // of the row in this workgroup
+    for (int s2 = slot + 1; s2 < kSlots && h.ends == 0; ++s2) more = more || heads_of[s2].ends >= 0;
+    if (more) continue;
+    open = false;
+    const bool mine_too = c < h.heads;
+    if (begun && h.ends == 1) {
+      if (mine_too) put_output<kType, kWidth>(a, out, lse, h.r, h.first + c, d, sums.o, sums.m, sums.l);
+    } else {
+      if (mine_too) {
+        const int at = (2 * w + (begun ? 1 : 0)) * piece_heads(a) + c;
+        if (d == 0) pc.ml[at] = float2{sums.m, sums.l};
+#pragma unroll
+        for (int i = 0; i < kWidth; i += 4)
+          *reinterpret_cast<f32x4*>(pc.o + (int64_t)at * kDim + d + i) = f32x4{sums.o[i], sums.o[i + 1], sums.o[i + 2], sums.o[i + 3]};
+      }
+      if (begun && threadIdx.x == 0) {
+        const int64_t end = run_start(total, (w + 1) * kGroupWaves) + h.behind - 1;  // the row's last tile
+        pc.cut[w] = int4{h.r, h.first | h.heads << 16, w, run_of(total, end) / kGroupWaves};
+      }
+    }
+  }
+  zero_rows<kType, kDim>(a, lengths, out, lse, w);
+}
+
+// The rows that fell to several workgroups, in the order of these: one workgroup per
+// such row and query; its 16-byte lanes take kThreads * 4 / kDim pieces at a time.
 template <int kType, int kDim>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const void* __restrict__ workspace, char* __restrict__ out,
                                                               float* __restrict__ lse, DecodeArgs a) {
   constexpr int kLanes = kDim / 4, kAtOnce = kThreads / kLanes;
-  __shared__ f32x4 part[kAtOnce][kLanes];
+  __shared__ float part[kAtOnce][kDim];
   __shared__ float2 part_ml[kAtOnce];
   const Pieces pc = pieces(const_cast<void*>(workspace), piece_heads(a));
   const int4 cut = pc.cut[blockIdx.x];
   if (cut.z < 0) return;
-  const int qt = cut.y % a.qtiles, n = blockIdx.y;
-  if (n >= min(a.group - 16 * qt, 16)) return;
-  const int head = cut.y / a.qtiles * a.group + 16 * qt + n;
-  const int slot = threadIdx.x / kLanes, d = threadIdx.x % kLanes;
+  const int n = blockIdx.y;
+  if (n >= cut.y >> 16) return;
+  const int slot = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
   const int count = cut.w - cut.z + 1;
-  float m = -INFINITY, l = 0.0f;
-  f32x4 o{0, 0, 0, 0};
+  Sums<4> sums;
+  sums.clear();
   for (int i = slot; i < count; i += kAtOnce) {
     const int at = (2 * (cut.z + i) + (i == 0 ? 1 : 0)) * piece_heads(a) + n;
-    const float2 ml = pc.ml[at];
-    const f32x4 x = *reinterpret_cast<const f32x4*>(pc.o + (int64_t)at * kDim + 4 * d);
-    const float to = fmaxf(m, ml.x);
-    const float f = to == -INFINITY ? 1.0f : exp2_fast(m - to), g = to == -INFINITY ? 1.0f : exp2_fast(ml.x - to);
-    o = o * f + x * g;
-    l = l * f + ml.y * g;
-    m = to;
+    const f32x4 x = *reinterpret_cast<const f32x4*>(pc.o + (int64_t)at * kDim + d);
+    const float y[4] = {x[0], x[1], x[2], x[3]};
+    sums.add(y, pc.ml[at]);
   }
-  part[slot][d] = o;
-  if (d == 0) part_ml[slot] = float2{m, l};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) part[slot][d + i] = sums.o[i];
+  if (d == 0) part_ml[slot] = float2{sums.m, sums.l};
   __syncthreads();
   if (slot > 0) return;
 #pragma unroll
-  for (int i = 1; i < kAtOnce; ++i) {
-    const float2 ml = part_ml[i];
-    const float to = fmaxf(m, ml.x);
-    const float f = to == -INFINITY ? 1.0f : exp2_fast(m - to), g = to == -INFINITY ? 1.0f : exp2_fast(ml.x - to);
-    o = o * f + part[i][d] * g;
-    l = l * f + ml.y * g;
-    m = to;
-  }
-  o *= l > 0.0f ? 1.0f / l : l;
-  const int64_t to = head * a.out_head + cut.x * a.out_request + 4 * d;
-  if constexpr (kType == 0)
-    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + to) = o;
-  else
-    *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(out) + to) = u32x2{bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};
-  if (lse && d == 0) lse[(int64_t)head * a.requests + cut.x] = (m + __log2f(l)) * kLn2;
+  for (int i = 1; i < kAtOnce; ++i) sums.add(&part[i][d], part_ml[i]);
+  put_output<kType, 4>(a, out, lse, cut.x, (cut.y & 0xffff) + n, d, sums.o, sums.m, sums.l);
 }
+
+// --------------------------------------------------------------- whole rows
+
+// One workgroup per row: its waves take equal runs of the row's tiles and add up in
+// LDS. No counting, no pieces, no second launch.
+template <int kType, int kDim>
+__global__ __launch_bounds__(kRowThreads, 2) void paged_rows_kernel(
+    const char* __restrict__ q, const char* __restrict__ k, const char* __restrict__ v,
+    const uint8_t* __restrict__ k_exp, const uint8_t* __restrict__ v_exp, const int32_t* __restrict__ table,
+    const int32_t* __restrict__ lengths, char* __restrict__ out, float* __restrict__ lse, DecodeArgs a) {
+  using S = Shape<kType, kDim>;
+  __shared__ Parts<kDim> lds;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = a.kv_heads * a.qtiles;
+  Place<S::kGroups> next;
+  next.r = blockIdx.x / rows;
+  next.h = (blockIdx.x - next.r * rows) / a.qtiles;
+  next.qt = blockIdx.x - next.r * rows - next.h * a.qtiles;
+  next.set_row(a);
+  next.s = span_of<S::kTile>(a, lengths[next.r]);
+  const int32_t lo = (int32_t)((int64_t)next.s.count * wave / kRowWaves), hi = (int32_t)((int64_t)next.s.count * (wave + 1) / kRowWaves);
+  next.x = lo;
+  State<kType, kDim> none;
+  none.m = -INFINITY;
+  none.l = 0.0f;
+#pragma unroll
+  for (int i = 0; i < S::kVDims; ++i) none.o[i] = f32x4{0, 0, 0, 0};
+  const int r = next.r, first = next.first, heads = next.heads;
+  if (lo < hi)
+    walk<kType, kDim>(
+        a, q, k, v, k_exp, v_exp, table, next, hi - lo,
+        [&](Place<S::kGroups>& p) {
+          ++p.x;
+          return false;
+        },
+        [&](const State<kType, kDim>& st, const Place<S::kGroups>&, bool, bool) { put_part<kType, kDim>(lds, wave, st); });
+  else
+    put_part<kType, kDim>(lds, wave, none);
+  __syncthreads();
+  constexpr int kWidth = kDim * 16 / kRowThreads;
+  const int c = threadIdx.x >> 5, d = (threadIdx.x & 31) * kWidth;
+  if (c >= heads) return;
+  Sums<kWidth> sums;
+  sums.clear();
+#pragma unroll
+  for (int i = 0; i < kRowWaves; ++i) sums.add(&lds.o[i][c][d], lds.ml[i][c]);
+  put_output<kType, kWidth>(a, out, lse, r, first + c, d, sums.o, sums.m, sums.l);
+}
+
+// Rows are not shared out where the longest that the table has room for (the
+// lengths themselves are the GPU's) is this short: us, whole rows / shared out, 8
+// rows of four query heads at 128, 256, 512 KB: bf16 of dimension 64 6.0 / 10.9,
+// 8.6 / 11.0, 13.7 / 10.9; of dimension 128 5.9 / 9.9, 8.3 / 11.0, 12.6 / 11.1; fp32
+// 6.8 / 10.9, 10.1 / 12.6, 16.2 / 12.7; 8 bits 7.1 / 11.9, 10.9 / 12.9, 16.8 / 13.1;
+// 1024 rows at 256 and 512 KB: 33 / 38, 59 / 62 (bf16, 64). Shared out costs a
+// second launch, about 6 us of the host's time.
+constexpr int64_t kWholeRowBytes = 384 << 10;
+bool whole_rows(int size, int dim, const DecodeArgs& a) {
+  return (int64_t)a.max_pages * a.page.size * dim * size * 2 <= kWholeRowBytes;
+}
+int value_size(int dtype) { return dtype == 0 ? 4 : dtype == 1 ? 2 : 1; }
 
 template <int kType, int kDim>
 hipError_t launch(const void* q, const void* kp, const void* vp, const uint8_t* ke, const uint8_t* ve, const int32_t* table,
                   const int32_t* lengths, void* out, float* lse, void* workspace, const DecodeArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((paged_attention_kernel<kType, kDim>), dim3(kWaves / (kThreads / 64)), dim3(kThreads), 0, s,
+  if (whole_rows(value_size(kType), kDim, a)) {
+    hipLaunchKernelGGL((paged_rows_kernel<kType, kDim>), dim3((unsigned)(a.requests * a.kv_heads * a.qtiles)), dim3(kRowThreads),
+                       0, s, static_cast<const char*>(q), static_cast<const char*>(kp), static_cast<const char*>(vp), ke, ve,
+                       table, lengths, static_cast<char*>(out), lse, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((paged_attention_kernel<kType, kDim>), dim3(kWorkgroups), dim3(kThreads), 0, s,
                      static_cast<const char*>(q), static_cast<const char*>(kp), static_cast<const char*>(vp), ke, ve, table,
                      lengths, static_cast<char*>(out), lse, workspace, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_join_kernel<kType, kDim>), dim3(kWaves, (unsigned)piece_heads(a)), dim3(kThreads), 0, s, workspace,
+  hipLaunchKernelGGL((paged_join_kernel<kType, kDim>), dim3(kWorkgroups, (unsigned)piece_heads(a)), dim3(kThreads), 0, s, workspace,
                      static_cast<char*>(out), lse, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t paged_attention_workspace(int dim, const DecodeArgs& a) {
-  return kCutBytes + (int64_t)2 * kWaves * piece_heads(a) * ((int64_t)sizeof(float2) + dim * (int64_t)sizeof(float));
+int64_t paged_attention_workspace(int dtype, int dim, const DecodeArgs& a) {
+  if (whole_rows(value_size(dtype), dim, a)) return 0;
+  return kCutBytes + (int64_t)2 * kWorkgroups * piece_heads(a) * ((int64_t)sizeof(float2) + dim * (int64_t)sizeof(float));
 }
 
 hipError_t launch_paged_attention(int dtype, int dim, const void* q, const void* k_pages,

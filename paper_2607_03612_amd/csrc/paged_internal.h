@@ -34,17 +34,19 @@ struct StepArgs {
   int32_t max_pages;
   int32_t pages;
   int32_t tokens;
+  int32_t in_place;
   PageDiv page;
 };
 
 // What the slot pass needs of a request.
 struct RequestRecord {
-  int32_t start;   // its first new token's place
   int32_t length;  // tokens before the step
   int32_t top;     // stack index of the first page it takes (the next ones lie below), -1 if refused
   int32_t held;    // pages before the step
 };
 
+// Whether a step is one launch, without a workspace.
+bool page_tables_in_one(int32_t requests, int32_t tokens, bool in_place);
 hipError_t launch_page_tables(const int32_t* lengths, const int32_t* new_tokens, int32_t* free_pages,
                               const int32_t* free_count, int32_t* table, int32_t* lengths_out,
                               int32_t* count_out, int32_t* start, int32_t* slots,
@@ -88,6 +90,6 @@ hipError_t launch_paged_attention(int dtype, int dim, const void* q, const void*
                                   const void* v_pages, const uint8_t* k_exp, const uint8_t* v_exp,
                                   const int32_t* table, const int32_t* lengths, void* out, float* lse,
                                   void* workspace, const DecodeArgs& a, hipStream_t s);
-int64_t paged_attention_workspace(int dim, const DecodeArgs& a);
+int64_t paged_attention_workspace(int dtype, int dim, const DecodeArgs& a);
 
 }  // namespace saf3r

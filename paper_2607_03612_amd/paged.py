@@ -26,7 +26,7 @@ _INT_MAX = 2 ** 31 - 1
 
 
 class PageStep(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("requests", "page_size", "max_pages", "pages", "tokens")]
+    _fields_ = [(n, ctypes.c_int32) for n in ("requests", "page_size", "max_pages", "pages", "tokens", "in_place")]
 
 
 class PageLayout(ctypes.Structure):
@@ -60,37 +60,33 @@ def _declare(lib):
     return lib
 
 
-_DECLARED = None
+torch = None  # with the library, by _lib(), which every call goes through first
+_LIB = None
+_TYPES = {}  # of a cache: its code, and the type of tokens, queries and outputs
 
 
 def _lib():
-    global _DECLARED
-    lib = binding.load()
-    if _DECLARED is not lib:
-        _DECLARED = _declare(lib)
-    return lib
+    global torch, _LIB
+    if _LIB is None or _LIB is not binding._LIB:
+        import torch as module
+
+        torch = module
+        _TYPES.update({torch.float32: (binding.F32, torch.float32), torch.bfloat16: (binding.BF16, torch.bfloat16),
+                       torch.float8_e4m3fn: (E4M3, torch.bfloat16)})
+        _LIB = _declare(binding.load())
+    return _LIB
 
 
-class _Call:
-    """Device and stream of a call: the tensors' device is made current for it
-    where it is not, and the stream is the device's current one by default."""
-
-    def __init__(self, device, stream):
-        import torch
-
-        self.device, self.given = device, stream
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-    def __enter__(self):
-        import torch
-
-        if self.guard is not None:
-            self.guard.__enter__()
-        return (torch.cuda.current_stream() if self.given is None else self.given).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _call(function, device, stream, *args):
+    """``function(*args, stream)`` with the tensors' device current, on the stream
+    given or the device's current one; its status is checked."""
+    if device.index != torch._C._cuda_getDevice():
+        with torch.cuda.device(device):
+            return _call(function, device, stream, *args)
+    # the handle alone: a Stream object takes 2.6 us
+    status = function(*args, torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream)
+    if status != 0:
+        raise Saf3rError(status, function.__name__)
 
 
 def _check_int(name, x, low):
@@ -99,28 +95,32 @@ def _check_int(name, x, low):
 
 
 def _check_words(name, t, shape, device):
-    import torch
-
-    if not (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.shape == shape and t.device == device):
-        raise ValueError(f"{name} must be a contiguous int32 device tensor of shape {list(shape)} on {device}")
+    if t.dtype != torch.int32 or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {list(shape)} on {device}")
 
 
-def _workspace(nbytes, device, stream):
-    import torch
+def _check_device(device):
+    if device.type != "cuda":
+        raise ValueError("expected device tensors")
 
-    t = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
-    binding._keep_until_done(stream, t)
-    return t
+
+def _allocated(stream, *tensors):
+    """Memory of the current stream that the call allocated, for use on `stream`:
+    not before the current stream is done with what lay there, and not handed out
+    again before `stream` is."""
+    if stream is not None and any(t is not None for t in tensors):
+        binding._after_current(stream)
+        binding._keep_until_done(stream, *(t for t in tensors if t is not None))
 
 
 def _given_workspace(t, device):
-    if not (t.is_cuda and t.is_contiguous() and t.device == device):
-        raise ValueError(f"the workspace must be a contiguous device tensor on {device}")
+    if not t.is_contiguous() or t.device != device:
+        raise ValueError(f"the workspace must be a contiguous tensor on {device}")
     return t.numel() * t.element_size()
 
 
-def page_tables_workspace_bytes(requests, page_size, max_pages, pages, tokens) -> int:
-    step = PageStep(requests, page_size, max_pages, pages, tokens)
+def page_tables_workspace_bytes(requests, page_size, max_pages, pages, tokens, in_place=False) -> int:
+    step = PageStep(requests, page_size, max_pages, pages, tokens, int(in_place))
     r = _lib().saf3r_page_tables_workspace_bytes(ctypes.byref(step))
     binding._check(min(r, 0), "saf3r_page_tables_workspace_bytes")
     return int(r)
@@ -138,70 +138,75 @@ def page_tables(lengths, new_tokens, free_pages, free_count, page_table, page_si
     in the order of the requests. A request that does not fit keeps its length,
     and its slots are -1. ``lengths_out`` may be ``lengths`` and ``free_count_out``
     ``free_count``."""
-    import torch
-
+    lib = _lib()
     _check_int("page_size", page_size, 1)
     _check_int("tokens", tokens, 0)
     dev = lengths.device
-    R = lengths.shape[0]
+    _check_device(dev)
+    if lengths.dim() != 1 or free_pages.dim() != 1 or page_table.dim() != 2:
+        raise ValueError("lengths must be [requests], free_pages [pages] and page_table [requests, max_pages]")
+    R, width, pages = lengths.shape[0], page_table.shape[1], free_pages.shape[0]
     _check_words("lengths", lengths, (R,), dev)
     _check_words("new_tokens", new_tokens, (R,), dev)
-    if free_pages.dim() != 1 or page_table.dim() != 2:
-        raise ValueError("free_pages must be [pages] and page_table [requests, max_pages]")
-    _check_words("free_pages", free_pages, free_pages.shape, dev)
+    _check_words("free_pages", free_pages, (pages,), dev)
     _check_words("free_count", free_count, (1,), dev)
-    _check_words("page_table", page_table, (R, page_table.shape[1]), dev)
-    outs = []
+    _check_words("page_table", page_table, (R, width), dev)
+    outs, made = [], []
     for name, t, n in (("lengths_out", lengths_out, R), ("token_start", token_start, R + 1), ("slots", slots, tokens),
                        ("free_count_out", free_count_out, 1)):
         if t is None:
             t = torch.empty(n, dtype=torch.int32, device=dev)
+            made.append(t)
         else:
             _check_words(name, t, (n,), dev)
         outs.append(t)
-    step = PageStep(R, page_size, page_table.shape[1], free_pages.shape[0], tokens)
+    lengths_at, count_at = lengths.data_ptr(), free_count.data_ptr()
+    lengths_to, count_to = outs[0].data_ptr(), outs[3].data_ptr()
+    step = PageStep(R, page_size, width, pages, tokens, 1 if lengths_at == lengths_to or count_at == count_to else 0)
     if workspace is None:
-        nbytes = 16 * R
-        workspace = _workspace(nbytes, dev, stream)
+        nbytes = lib.saf3r_page_tables_workspace_bytes(ctypes.byref(step))
+        binding._check(min(nbytes, 0), "saf3r_page_tables")
+        if nbytes > 0:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            made.append(workspace)
     else:
         nbytes = _given_workspace(workspace, dev)
-    with _Call(dev, stream) as st:
-        binding._check(_lib().saf3r_page_tables(
-            ctypes.byref(step), lengths.data_ptr(), new_tokens.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
-            page_table.data_ptr(), outs[0].data_ptr(), outs[3].data_ptr(), outs[1].data_ptr(), outs[2].data_ptr(),
-            workspace.data_ptr(), nbytes, st), "saf3r_page_tables")
+    if stream is not None:
+        _allocated(stream, *made)
+    _call(lib.saf3r_page_tables, dev, stream, ctypes.byref(step), lengths_at, new_tokens.data_ptr(), free_pages.data_ptr(),
+          count_at, page_table.data_ptr(), lengths_to, count_to, outs[1].data_ptr(), outs[2].data_ptr(), _ptr(workspace), nbytes)
     return tuple(outs)
 
 
 def _layout(k_pages, v_pages, k_exp, v_exp):
     """The pages' layout, and the type of tokens and queries beside them."""
-    import torch
-
-    kind = torch.bfloat16
-    if k_pages.dtype == torch.float8_e4m3fn:
-        code = E4M3
-    else:
-        code = binding._torch_dtype_code(k_pages)
-        kind = k_pages.dtype
-    if not (k_pages.is_cuda and k_pages.dim() == 4 and k_pages.stride(3) == 1):
-        raise ValueError("pages must be device tensors [pages, kv_heads, page_size, head_dim], head_dim contiguous")
-    if v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype or v_pages.device != k_pages.device \
-            or v_pages.stride() != k_pages.stride():
+    dtype, dev, shape, strides = k_pages.dtype, k_pages.device, k_pages.shape, k_pages.stride()
+    if dtype not in _TYPES:
+        raise ValueError(f"unsupported cache dtype {dtype}")
+    code, kind = _TYPES[dtype]
+    _check_device(dev)
+    if len(shape) != 4 or strides[3] != 1:
+        raise ValueError("pages must be [pages, kv_heads, page_size, head_dim], head_dim contiguous")
+    if v_pages.shape != shape or v_pages.dtype != dtype or v_pages.device != dev or v_pages.stride() != strides:
         raise ValueError("k_pages and v_pages must share shape, strides, dtype and device")
-    n, H, ps, D = k_pages.shape
+    n, H, ps, D = shape
     if code == E4M3:
         for t in (k_exp, v_exp):
-            if t is None or not (t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous() and t.shape == (n, H, ps)
-                                 and t.device == k_pages.device):
+            if t is None or t.dtype != torch.uint8 or not t.is_contiguous() or t.shape != (n, H, ps) or t.device != dev:
                 raise ValueError("an e4m3 cache needs k_exp and v_exp, contiguous uint8 [pages, kv_heads, page_size]")
     elif k_exp is not None or v_exp is not None:
         raise ValueError("k_exp and v_exp belong to an e4m3 cache")
-    sp, sh, st, _ = k_pages.stride()
-    return PageLayout(n, ps, H, D, code, 0, sp, sh, st), kind
+    return PageLayout(n, ps, H, D, code, 0, strides[0], strides[1], strides[2]), kind
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _check_apart(name, t):
+    """Entries that a call writes must not share memory."""
+    if 0 in t.stride() and any(s == 0 and n > 1 for s, n in zip(t.stride(), t.shape)):
+        raise ValueError(f"{name} must not share memory among their entries")
 
 
 def cache_append(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=None):
@@ -211,28 +216,28 @@ def cache_append(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=N
     fp32 tokens into an fp32 cache, bf16 ones into a bf16 or ``float8_e4m3fn``
     one, the latter with the exponents ``k_exp`` and ``v_exp``. Slots outside the
     cache (-1) are skipped; the others must be distinct."""
+    lib = _lib()
     layout, kind = _layout(k_pages, v_pages, k_exp, v_exp)
-    H, T, D = k.shape
-    if not (k.is_cuda and k.dtype == kind and k.stride(2) == 1 and k.device == k_pages.device):
-        raise ValueError(f"k and v must be {kind} tensors on {k_pages.device}, head_dim contiguous")
-    if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device or v.stride() != k.stride():
+    dev, shape, strides = k.device, k.shape, k.stride()
+    if k.dtype != kind or dev != k_pages.device or len(shape) != 3 or strides[2] != 1:
+        raise ValueError(f"k and v must be {kind} tensors [kv_heads, tokens, head_dim] on {k_pages.device}, head_dim contiguous")
+    if v.shape != shape or v.dtype != kind or v.device != dev or v.stride() != strides:
         raise ValueError("k and v must share shape, strides, dtype and device")
+    H, T, D = shape
     if H != layout.kv_heads or D != layout.head_dim:
-        raise ValueError("k and v must be [kv_heads, tokens, head_dim] with the cache's kv_heads and head_dim")
-    if any(s == 0 and n > 1 for s, n in zip(k_pages.stride(), k_pages.shape)):
-        raise ValueError("the pages' entries must not share memory")
-    _check_words("slots", slots, (T,), k.device)
-    rows = TokenLayout(T, 0, k.stride(0), k.stride(1))
-    with _Call(k.device, stream) as st:
-        binding._check(_lib().saf3r_cache_append(
-            ctypes.byref(layout), ctypes.byref(rows), k.data_ptr(), v.data_ptr(), slots.data_ptr(), k_pages.data_ptr(),
-            v_pages.data_ptr(), _ptr(k_exp), _ptr(v_exp), st), "saf3r_cache_append")
+        raise ValueError("k and v must have the cache's kv_heads and head_dim")
+    _check_apart("the pages", k_pages)
+    _check_words("slots", slots, (T,), dev)
+    rows = TokenLayout(T, 0, strides[0], strides[1])
+    _call(lib.saf3r_cache_append, dev, stream, ctypes.byref(layout), ctypes.byref(rows), k.data_ptr(), v.data_ptr(),
+          slots.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_exp), _ptr(v_exp))
 
 
 def paged_attention_workspace_bytes(q, k_pages, v_pages, page_table, k_exp=None, v_exp=None) -> int:
+    lib = _lib()
     layout, _ = _layout(k_pages, v_pages, k_exp, v_exp)
     step = Decode(q.shape[1], q.shape[0], page_table.shape[1], 0, 0, 1.0, 0, 0, 0, 0)
-    r = _lib().saf3r_paged_attention_workspace_bytes(ctypes.byref(layout), ctypes.byref(step))
+    r = lib.saf3r_paged_attention_workspace_bytes(ctypes.byref(layout), ctypes.byref(step))
     binding._check(min(r, 0), "saf3r_paged_attention_workspace_bytes")
     return int(r)
 
@@ -247,38 +252,42 @@ def paged_attention(q, k_pages, v_pages, page_table, lengths, k_exp=None, v_exp=
     kv_heads)``. ``lengths [requests]`` tokens are attended, with ``window > 0``
     only the first ``anchor`` and the last ``window`` of them; a request without a
     token gives zeros and -inf. ``scale`` is ``head_dim ** -0.5`` by default."""
-    import torch
-
+    lib = _lib()
     _check_int("anchor", anchor, 0)
     _check_int("window", window, 0)
     layout, kind = _layout(k_pages, v_pages, k_exp, v_exp)
-    dev = k_pages.device
-    Hq, R, D = q.shape
-    if not (q.is_cuda and q.dtype == kind and q.stride(2) == 1 and q.device == dev and D == layout.head_dim):
+    dev, shape, strides = k_pages.device, q.shape, q.stride()
+    if q.dtype != kind or q.device != dev or len(shape) != 3 or strides[2] != 1 or shape[2] != layout.head_dim:
         raise ValueError(f"q must be a {kind} tensor [q_heads, requests, {layout.head_dim}] on {dev}, head_dim contiguous")
+    Hq, R, D = shape
     if page_table.dim() != 2:
         raise ValueError("page_table must be [requests, max_pages]")
-    _check_words("page_table", page_table, (R, page_table.shape[1]), dev)
+    width = page_table.shape[1]
+    _check_words("page_table", page_table, (R, width), dev)
     _check_words("lengths", lengths, (R,), dev)
+    made = []
     if out is None:
         out = torch.empty_like(q)
-    elif not (out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.stride(2) == 1):
-        raise ValueError("out must be like q, head_dim contiguous")
-    if any(s == 0 and n > 1 for s, n in zip(out.stride(), out.shape)):
-        raise ValueError("the rows of out must not share memory")
+        made.append(out)
+    elif out.shape != shape or out.dtype != kind or out.device != dev:
+        raise ValueError("out must be like q")
+    to = out.stride()
+    if to[2] != 1:
+        raise ValueError("out's head_dim must be contiguous")
+    _check_apart("the rows of out", out)
     lse = torch.empty((Hq, R), dtype=torch.float32, device=dev) if want_lse else None
-    step = Decode(R, Hq, page_table.shape[1], anchor, window, D ** -0.5 if scale is None else scale, q.stride(0),
-                  q.stride(1), out.stride(0), out.stride(1))
-    lib = _lib()
+    step = Decode(R, Hq, width, anchor, window, D ** -0.5 if scale is None else scale, strides[0], strides[1], to[0], to[1])
     if workspace is None:
         nbytes = lib.saf3r_paged_attention_workspace_bytes(ctypes.byref(layout), ctypes.byref(step))
         binding._check(min(nbytes, 0), "saf3r_paged_attention")
-        workspace = _workspace(nbytes, dev, stream)
+        if nbytes > 0:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            made.append(workspace)
     else:
         nbytes = _given_workspace(workspace, dev)
-    with _Call(dev, stream) as st:
-        binding._check(lib.saf3r_paged_attention(
-            ctypes.byref(layout), ctypes.byref(step), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_exp),
-            _ptr(v_exp), page_table.data_ptr(), lengths.data_ptr(), out.data_ptr(), _ptr(lse), workspace.data_ptr(),
-            nbytes, st), "saf3r_paged_attention")
+    if stream is not None:
+        _allocated(stream, lse, *made)
+    _call(lib.saf3r_paged_attention, dev, stream, ctypes.byref(layout), ctypes.byref(step), q.data_ptr(), k_pages.data_ptr(),
+          v_pages.data_ptr(), _ptr(k_exp), _ptr(v_exp), page_table.data_ptr(), lengths.data_ptr(), out.data_ptr(), _ptr(lse),
+          _ptr(workspace), nbytes)
     return out, lse
