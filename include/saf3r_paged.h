@@ -27,8 +27,8 @@
  * entry gives no access outside the arrays, as each call says.
  *
  * The cache: K pages and V pages, each [pages][kv_heads][page_size][head_dim]
- * addressed by the strides of saf3r_page_layout (the same for both, head_dim
- * contiguous), so token-major pages do as well. Slot s is token s % page_size of
+ * addressed by the strides of a saf3r_page_layout, the same for both, with head_dim
+ * contiguous; so token-major pages do as well. Slot s is token s % page_size of
  * page s / page_size. Element types:
  *   SAF3R_CACHE_F32   fp32, with fp32 tokens, queries and outputs;
  *   SAF3R_CACHE_BF16  bf16, with bf16 ones;

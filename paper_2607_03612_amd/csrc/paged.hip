@@ -5,11 +5,6 @@ namespace saf3r {
 namespace {
 
 constexpr int kSlotThreads = 256;
-// Steps of up to so many requests are one launch (see page_step_kernel), of as many
-// workgroups as it takes to give each thread kSlotsEach new tokens.
-constexpr int kStepRequests = 1024;
-constexpr int kSlotsEach = 4;
-
 // Sums stop at a limit of at most 2^30 + 1: a + b fits 32 bits, and the order
 // of additions does not matter.
 __device__ inline uint32_t add_to(uint32_t a, uint32_t b, uint32_t limit) { return min(a + b, limit); }
@@ -332,11 +327,6 @@ hipError_t append(const void* k, const void* v, const int32_t* slots, void* kp, 
 }
 
 }  // namespace
-
-bool page_tables_in_one(int32_t requests, int32_t tokens, bool in_place) {
-  // in place, the workgroups of one launch would read what its first one writes
-  return requests <= kStepRequests && (!in_place || tokens <= kStepRequests * kSlotsEach);
-}
 
 hipError_t launch_page_tables(const int32_t* lengths, const int32_t* new_tokens, int32_t* free_pages,
                               const int32_t* free_count, int32_t* table, int32_t* lengths_out,

@@ -22,17 +22,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// Shared-out launches: 512 workgroups of four waves, two waves to a SIMD. Each wave
-// takes the same number of tiles, at least kMinTiles, so that a short launch does
-// not spend itself on joining.
-constexpr int kThreads = 256;
-constexpr int kGroupWaves = kThreads / 64;
-constexpr int kWorkgroups = 512;
-constexpr int kWaves = kWorkgroups * kGroupWaves;  // a power of two
-constexpr int kMinTiles = 2;
-// Whole-row launches: eight waves share a row.
-constexpr int kRowThreads = 512;
-constexpr int kRowWaves = kRowThreads / 64;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // kType: 0 fp32, 1 bf16, 2 e4m3.
@@ -585,8 +574,6 @@ struct Pieces {
   int4* cut;   // a row that begins in workgroup w and ends in a later one: (request, first query head and, from
                // bit 16 on, their number, w, last one), else z < 0
 };
-constexpr int64_t kCutBytes = (int64_t)kWorkgroups * sizeof(int4);
-
 __host__ __device__ inline Pieces pieces(void* workspace, int heads) {
   Pieces p;
   p.cut = static_cast<int4*>(workspace);
@@ -594,8 +581,6 @@ __host__ __device__ inline Pieces pieces(void* workspace, int heads) {
   p.o = reinterpret_cast<float*>(p.ml + 2 * kWorkgroups * heads);
   return p;
 }
-__host__ __device__ inline int piece_heads(const DecodeArgs& a) { return a.group < 16 ? a.group : 16; }
-
 // The next request after r that has tiles (64 lengths at a time), or `requests`.
 __device__ inline int next_request(const DecodeArgs& a, const int32_t* __restrict__ lengths, int r) {
   const int lane = threadIdx.x & 63;
@@ -856,23 +841,10 @@ __global__ __launch_bounds__(kRowThreads, 2) void paged_rows_kernel(
   put_output<kType, kWidth>(a, out, lse, r, first + c, d, sums.o, sums.m, sums.l);
 }
 
-// Rows are not shared out where the longest that the table has room for (the
-// lengths themselves are the GPU's) is this short: us, whole rows / shared out, 8
-// rows of four query heads at 128, 256, 512 KB: bf16 of dimension 64 6.0 / 10.9,
-// 8.6 / 11.0, 13.7 / 10.9; of dimension 128 5.9 / 9.9, 8.3 / 11.0, 12.6 / 11.1; fp32
-// 6.8 / 10.9, 10.1 / 12.6, 16.2 / 12.7; 8 bits 7.1 / 11.9, 10.9 / 12.9, 16.8 / 13.1;
-// 1024 rows at 256 and 512 KB: 33 / 38, 59 / 62 (bf16, 64). Shared out costs a
-// second launch, about 6 us of the host's time.
-constexpr int64_t kWholeRowBytes = 384 << 10;
-bool whole_rows(int size, int dim, const DecodeArgs& a) {
-  return (int64_t)a.max_pages * a.page.size * dim * size * 2 <= kWholeRowBytes;
-}
-int value_size(int dtype) { return dtype == 0 ? 4 : dtype == 1 ? 2 : 1; }
-
 template <int kType, int kDim>
 hipError_t launch(const void* q, const void* kp, const void* vp, const uint8_t* ke, const uint8_t* ve, const int32_t* table,
                   const int32_t* lengths, void* out, float* lse, void* workspace, const DecodeArgs& a, hipStream_t s) {
-  if (whole_rows(value_size(kType), kDim, a)) {
+  if (whole_rows(kType, kDim, a)) {
     hipLaunchKernelGGL((paged_rows_kernel<kType, kDim>), dim3((unsigned)(a.requests * a.kv_heads * a.qtiles)), dim3(kRowThreads),
                        0, s, static_cast<const char*>(q), static_cast<const char*>(kp), static_cast<const char*>(vp), ke, ve,
                        table, lengths, static_cast<char*>(out), lse, a);
@@ -889,11 +861,6 @@ hipError_t launch(const void* q, const void* kp, const void* vp, const uint8_t* 
 }
 
 }  // namespace
-
-int64_t paged_attention_workspace(int dtype, int dim, const DecodeArgs& a) {
-  if (whole_rows(value_size(dtype), dim, a)) return 0;
-  return kCutBytes + (int64_t)2 * kWorkgroups * piece_heads(a) * ((int64_t)sizeof(float2) + dim * (int64_t)sizeof(float));
-}
 
 hipError_t launch_paged_attention(int dtype, int dim, const void* q, const void* k_pages,
                                   const void* v_pages, const uint8_t* k_exp, const uint8_t* v_exp,

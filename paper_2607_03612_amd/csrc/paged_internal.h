@@ -45,8 +45,14 @@ struct RequestRecord {
   int32_t held;    // pages before the step
 };
 
-// Whether a step is one launch, without a workspace.
-bool page_tables_in_one(int32_t requests, int32_t tokens, bool in_place);
+// Steps of up to so many requests are one launch, without a workspace, of as many
+// workgroups as it takes to give each thread kSlotsEach new tokens. In place the
+// workgroups would read what the first one writes, so there only of one.
+constexpr int kStepRequests = 1024;
+constexpr int kSlotsEach = 4;
+inline bool page_tables_in_one(int32_t requests, int32_t tokens, bool in_place) {
+  return requests <= kStepRequests && (!in_place || tokens <= kStepRequests * kSlotsEach);
+}
 hipError_t launch_page_tables(const int32_t* lengths, const int32_t* new_tokens, int32_t* free_pages,
                               const int32_t* free_count, int32_t* table, int32_t* lengths_out,
                               int32_t* count_out, int32_t* start, int32_t* slots,
@@ -86,10 +92,43 @@ struct DecodeArgs {
   int64_t q_head, q_request, out_head, out_request;
 };
 
+// Shared-out launches: 512 workgroups of four waves, two waves to a SIMD. Each wave
+// takes the same number of tiles, at least kMinTiles, so that a short launch does
+// not spend itself on joining.
+constexpr int kThreads = 256;
+constexpr int kGroupWaves = kThreads / 64;
+constexpr int kWorkgroups = 512;
+constexpr int kWaves = kWorkgroups * kGroupWaves;  // a power of two
+constexpr int kMinTiles = 2;
+// Whole-row launches: eight waves share a row.
+constexpr int kRowThreads = 512;
+constexpr int kRowWaves = kRowThreads / 64;
+
+// Rows are not shared out where the longest that the table has room for (the
+// lengths themselves are the GPU's) is this short: us, whole rows / shared out, 8
+// rows of four query heads at 128, 256, 512 KB: bf16 of dimension 64 6.0 / 10.9,
+// 8.6 / 11.0, 13.7 / 10.9; of dimension 128 5.9 / 9.9, 8.3 / 11.0, 12.6 / 11.1; fp32
+// 6.8 / 10.9, 10.1 / 12.6, 16.2 / 12.7; 8 bits 7.1 / 11.9, 10.9 / 12.9, 16.8 / 13.1;
+// 1024 rows at 256 and 512 KB: 33 / 38, 59 / 62 (bf16, 64). Shared out costs a
+// second launch, about 6 us of the host's time.
+constexpr int64_t kWholeRowBytes = 384 << 10;
+inline bool whole_rows(int dtype, int dim, const DecodeArgs& a) {
+  const int size = dtype == 0 ? 4 : dtype == 1 ? 2 : 1;
+  return (int64_t)a.max_pages * a.page.size * dim * size * 2 <= kWholeRowBytes;
+}
+
+// Query heads of a row, and the workspace: an int4 per workgroup, and two parts of a
+// row each, of a float2 and dim sums per query head.
+__host__ __device__ inline int piece_heads(const DecodeArgs& a) { return a.group < 16 ? a.group : 16; }
+constexpr int64_t kCutBytes = (int64_t)kWorkgroups * sizeof(int4);
+inline int64_t paged_attention_workspace(int dtype, int dim, const DecodeArgs& a) {
+  if (whole_rows(dtype, dim, a)) return 0;
+  return kCutBytes + (int64_t)2 * kWorkgroups * piece_heads(a) * (int64_t)(sizeof(float2) + dim * sizeof(float));
+}
+
 hipError_t launch_paged_attention(int dtype, int dim, const void* q, const void* k_pages,
                                   const void* v_pages, const uint8_t* k_exp, const uint8_t* v_exp,
                                   const int32_t* table, const int32_t* lengths, void* out, float* lse,
                                   void* workspace, const DecodeArgs& a, hipStream_t s);
-int64_t paged_attention_workspace(int dtype, int dim, const DecodeArgs& a);
 
 }  // namespace saf3r

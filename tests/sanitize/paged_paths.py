@@ -1,0 +1,70 @@
+"""Calls of the paged cache's C ABI that pass validation, and its integer
+arithmetic, for the sanitizer build only (its launches are stand-ins). Run by
+tests/test_paged_cpu.py in a process with AddressSanitizer preloaded."""
+import ctypes
+import random
+
+import pytest
+
+from paper_2607_03612_amd import binding
+from paper_2607_03612_amd import paged as G
+
+OK = ctypes.c_void_p(0x10000)  # never dereferenced by the stand-ins
+OTHER = ctypes.c_void_p(0x20000)
+
+
+def lib():
+    return G._declare(binding.load())
+
+
+@pytest.mark.parametrize("size", list(range(16, 1025, 16)))
+def test_page_division_is_exact(size):
+    div = lib().saf3r_stub_div_page
+    rng = random.Random(size)
+    top = (1 << 29) + 1023
+    xs = [0, 1, size - 1, size, size + 1, top, top - 1] + [rng.randint(0, top) for _ in range(300)]
+    for _ in range(300):  # around multiples, and the largest of them
+        m = rng.randint(1, top // size) * size
+        xs += [m - 1, m, min(m + size - 1, top)]
+    m = top // size * size
+    for x in xs + [m - 1, m]:
+        assert div(size, x) == x // size, (size, x)
+
+
+@pytest.mark.parametrize("requests,tokens,in_place,launches", [
+    (1, 0, 0, 1), (1024, 1 << 30, 0, 1), (1024, 4096, 1, 1), (1024, 4097, 1, 2), (1025, 1, 0, 2), (65536, 1 << 30, 1, 2)])
+def test_page_tables(requests, tokens, in_place, launches):
+    step = G.PageStep(requests, 1024, 1 << 19, 2097151, tokens, in_place)
+    need = lib().saf3r_page_tables_workspace_bytes(ctypes.byref(step))
+    assert need == (0 if launches == 1 else 12 * requests)
+    call = lib().saf3r_page_tables
+    outs = (OK, OK) if in_place else (OTHER, OTHER)
+    args = [OK, OK, OK, OK, OK, *outs, OK, OK]
+    assert call(ctypes.byref(step), *args, OK, need, None) == 0
+    assert lib().saf3r_stub_paged_launches() == launches
+    if need == 0:
+        assert call(ctypes.byref(step), *args, None, 0, None) == 0
+    # in place only where the step says so
+    if not in_place:
+        assert call(ctypes.byref(step), OK, OK, OK, OK, OK, OK, OTHER, OK, OK, OK, need, None) == -1
+        assert call(ctypes.byref(step), OK, OK, OK, OK, OK, OTHER, OK, OK, OK, OK, need, None) == -1
+
+
+@pytest.mark.parametrize("dtype,size,dim,page,width,launches", [
+    (0, 4, 64, 64, 12, 1), (0, 4, 64, 64, 13, 2), (1, 2, 128, 16, 48, 1), (1, 2, 128, 16, 49, 2), (2, 1, 128, 1024, 1, 1),
+    (2, 1, 128, 1024, 2, 2), (1, 2, 64, 1024, 1 << 19, 2)])
+@pytest.mark.parametrize("heads", [(1, 1), (256, 1), (256, 256), (96, 2)])
+def test_attention(dtype, size, dim, page, width, launches, heads):
+    hq, hk = heads
+    layout = G.PageLayout(2097151 if page == 1024 else 9, page, hk, dim, dtype, 0, hk * page * dim, page * dim, dim)
+    step = G.Decode(65536, hq, width, 2 ** 31 - 1, 2 ** 31 - 1, 0.125, 65536 * dim, dim, dim, hq * dim)
+    need = lib().saf3r_paged_attention_workspace_bytes(ctypes.byref(layout), ctypes.byref(step))
+    assert need == (0 if launches == 1 else 512 * 16 + 1024 * min(hq // hk, 16) * (8 + 4 * dim))
+    exps = (OK, OK) if dtype == 2 else (None, None)
+    call = lib().saf3r_paged_attention
+    assert call(ctypes.byref(layout), ctypes.byref(step), OK, OK, OK, *exps, OK, OK, OK, OK, OK, need, None) == 0
+    assert lib().saf3r_stub_paged_launches() == launches
+    assert call(ctypes.byref(layout), ctypes.byref(step), OK, OK, OK, *exps, OK, OK, OK, None, None if need == 0 else OK, need,
+                None) == 0
+    rows = G.TokenLayout(1 << 30, 0, dim, 0)
+    assert lib().saf3r_cache_append(ctypes.byref(layout), ctypes.byref(rows), OK, OK, OK, OK, OK, *exps, None) == 0

@@ -1,0 +1,138 @@
+"""The paged key-value cache's C ABI rejects bad arguments with a status code before
+anything is launched (none of these calls reaches the GPU)."""
+import ctypes
+import os
+
+import pytest
+
+OK, A8, A2 = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x1008), ctypes.c_void_p(0x1002)  # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def G():
+    from paper_2607_03612_amd import binding, paged
+
+    if not os.path.exists(binding.LIB_PATH):
+        from paper_2607_03612_amd import build
+
+        build.build()
+    return paged
+
+
+def lib_of(G):
+    from paper_2607_03612_amd import binding
+
+    return G._declare(binding.load())
+
+
+def step(G, **kw):
+    d = dict(requests=4, page_size=16, max_pages=8, pages=100, tokens=64, in_place=0)
+    d.update(kw)
+    return G.PageStep(*(d[n] for n, _ in G.PageStep._fields_))
+
+
+def test_page_tables_refuses(G):
+    lib = lib_of(G)
+    size = lib.saf3r_page_tables_workspace_bytes
+    assert size(None) == -1
+    for kw, want in ((dict(), 0), (dict(requests=2000), 24000), (dict(requests=0), -1), (dict(max_pages=0), -1),
+                     (dict(pages=0), -1), (dict(tokens=-1), -1), (dict(page_size=0), -1), (dict(page_size=-16), -1),
+                     (dict(page_size=24), -2), (dict(page_size=8), -2), (dict(page_size=1040), -2), (dict(in_place=2), -1),
+                     (dict(requests=65537), -2), (dict(max_pages=(1 << 25) + 1), -2), (dict(pages=1 << 27), -2),
+                     (dict(tokens=(1 << 30) + 1), -2)):
+        assert size(ctypes.byref(step(G, **kw))) == want, kw
+    call = lib.saf3r_page_tables
+    big = step(G, requests=2000)
+    args = [OK, OK, OK, OK, OK, ctypes.c_void_p(0x2000), ctypes.c_void_p(0x3000), OK, OK]
+    for i in range(9):
+        for bad in (None, A2):
+            assert call(ctypes.byref(big), *args[:i], bad, *args[i + 1:], OK, 24000, None) == -1, (i, bad)
+    assert call(ctypes.byref(big), *args, None, 24000, None) == -1
+    assert call(ctypes.byref(big), *args, A8, 24000, None) == -1
+    assert call(ctypes.byref(big), *args, OK, 23999, None) == -3
+    assert call(ctypes.byref(big), *args, OK, -1, None) == -1
+    assert call(None, *args, OK, 24000, None) == -1
+    # outputs that are inputs, in a step that does not say so
+    assert call(ctypes.byref(big), OK, OK, OK, OK, OK, OK, A8, OK, OK, OK, 24000, None) == -1
+
+
+def layout(G, **kw):
+    d = dict(pages=10, page_size=16, kv_heads=2, head_dim=64, dtype=1, reserved=0, page_stride=2048, head_stride=1024,
+             token_stride=64)
+    d.update(kw)
+    return G.PageLayout(*(d[n] for n, _ in G.PageLayout._fields_))
+
+
+BAD_LAYOUTS = [(dict(pages=0), -1), (dict(kv_heads=0), -1), (dict(dtype=3), -1), (dict(dtype=-1), -1), (dict(reserved=1), -1),
+               (dict(page_size=0), -1), (dict(page_size=20), -2), (dict(page_size=2048), -2), (dict(head_dim=32), -2),
+               (dict(head_dim=96), -2), (dict(kv_heads=257), -2), (dict(pages=1 << 27), -2), (dict(page_stride=-64), -1),
+               (dict(page_stride=2044), -1), (dict(head_stride=1), -1), (dict(token_stride=68), -1), (dict(token_stride=-8), -1),
+               (dict(token_stride=1 << 26), -1), (dict(page_stride=1 << 60), -1), (dict(head_stride=2 ** 62), -1),
+               (dict(dtype=2, token_stride=72), -1), (dict(dtype=0, token_stride=66), -1)]
+
+
+def decode(G, **kw):
+    d = dict(requests=3, q_heads=4, max_pages=400, anchor=0, window=0, scale=0.125, q_head_stride=192, q_request_stride=64,
+             out_head_stride=64, out_request_stride=256)
+    d.update(kw)
+    return G.Decode(*(d[n] for n, _ in G.Decode._fields_))
+
+
+def test_attention_refuses(G):
+    lib = lib_of(G)
+    size = lib.saf3r_paged_attention_workspace_bytes
+    good = layout(G)
+    need = size(ctypes.byref(good), ctypes.byref(decode(G)))
+    assert need == 512 * 16 + 1024 * 2 * (8 + 64 * 4)
+    assert size(ctypes.byref(good), ctypes.byref(decode(G, max_pages=4))) == 0  # short rows are not shared out
+    assert size(None, ctypes.byref(decode(G))) == -1 and size(ctypes.byref(good), None) == -1
+    for kw, want in BAD_LAYOUTS:
+        assert size(ctypes.byref(layout(G, **kw)), ctypes.byref(decode(G))) == want, kw
+    for kw, want in ((dict(requests=0), -1), (dict(q_heads=0), -1), (dict(max_pages=0), -1), (dict(anchor=-1), -1),
+                     (dict(window=-1), -1), (dict(scale=0.0), -1), (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1),
+                     (dict(scale=float("inf")), -1), (dict(requests=65537), -2), (dict(q_heads=258), -2), (dict(q_heads=3), -2),
+                     (dict(q_heads=1), -2), (dict(max_pages=(1 << 25) + 1), -2), (dict(q_head_stride=-192), -1),
+                     (dict(q_request_stride=65), -1), (dict(out_head_stride=2 ** 62), -1), (dict(out_request_stride=4), -1)):
+        assert size(ctypes.byref(good), ctypes.byref(decode(G, **kw))) == want, kw
+    call = lib.saf3r_paged_attention
+    args = [OK, OK, OK, None, None, OK, OK, OK, OK]
+    names = "q k v ke ve table lengths out lse".split()
+
+    def run(workspace=OK, nbytes=need, lay=good, **kw):
+        a = [kw.get(n, x) for n, x in zip(names, args)]
+        return call(ctypes.byref(lay), ctypes.byref(decode(G)), *a, workspace, nbytes, None)
+
+    for n in ("q", "k", "v", "out"):
+        assert run(**{n: None}) == -1 and run(**{n: A8}) == -1, n
+    for n in ("table", "lengths"):
+        assert run(**{n: None}) == -1 and run(**{n: A2}) == -1, n
+    assert run(lse=A2) == -1
+    assert run(ke=OK) == -1 and run(ve=OK) == -1  # exponents of a cache that has none
+    eight = layout(G, dtype=2)
+    for kw in (dict(), dict(ke=OK), dict(ve=OK), dict(ke=A2, ve=OK), dict(ke=OK, ve=A2)):
+        assert run(lay=eight, **kw) == -1, kw
+    assert run(workspace=None) == -1 and run(workspace=A8) == -1 and run(nbytes=-1) == -1
+    assert run(nbytes=need - 1) == -3
+    assert run(lay=layout(G, head_dim=96)) == -2
+
+
+def test_append_refuses(G):
+    call = lib_of(G).saf3r_cache_append
+    args = [OK, OK, OK, OK, OK, None, None]
+
+    def run(lay=None, rows=(5, 0, 320, 64), **kw):
+        a = [kw.get(n, x) for n, x in zip("k v slots kp vp ke ve".split(), args)]
+        rows = None if rows is None else ctypes.byref(G.TokenLayout(*rows))
+        return call(ctypes.byref(lay or layout(G)), rows, *a, None)
+
+    for kw, want in BAD_LAYOUTS:
+        assert run(layout(G, **kw)) == want, kw
+    for rows, want in ((None, -1), ((-1, 0, 64, 64), -1), ((5, 1, 64, 64), -1), ((5, 0, -64, 64), -1), ((5, 0, 64, 60), -1),
+                       ((5, 0, 2 ** 62, 64), -1), ((5, 0, 64, 2 ** 50), -1), (((1 << 30) + 1, 0, 64, 64), -2)):
+        assert run(rows=rows) == want, rows
+    for n in ("k", "v", "kp", "vp"):
+        assert run(**{n: None}) == -1 and run(**{n: A8}) == -1, n
+    assert run(slots=None) == -1 and run(slots=A2) == -1
+    assert run(ke=OK) == -1 and run(layout(G, dtype=2), ke=OK) == -1 and run(layout(G, dtype=2), ke=A2, ve=OK) == -1
+    # nothing to write needs no tokens
+    assert run(rows=(0, 0, 64, 64), k=None, v=None, slots=None) == 0

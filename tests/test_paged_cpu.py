@@ -1,0 +1,174 @@
+"""The paged key-value cache without a GPU: the binding's refusals, the host layer
+under sanitizers, the compiled kernels, and the plain definition that the GPU tests
+compare with."""
+import ctypes
+import os
+import re
+import shutil
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged as O
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def G():
+    from paper_2607_03612_amd import binding, paged
+
+    if not os.path.exists(binding.LIB_PATH):
+        from paper_2607_03612_amd import build
+
+        build.build()
+    paged._lib()
+    return paged
+
+
+def test_library_exports_every_declared_symbol(G):
+    text = open(os.path.join(ROOT, "include", "saf3r_paged.h")).read()
+    names = set(re.findall(r"^\s*(?:const\s+)?[\w\s\*]*?\b(saf3r_\w+)\s*\(", text, re.M))
+    assert names == set(G.EXPORTS)
+    lib = ctypes.CDLL(__import__("paper_2607_03612_amd").binding.LIB_PATH)
+    for n in names:
+        assert hasattr(lib, n), n
+
+
+# ---------------------------------------------------- the binding's refusals
+
+
+def test_binding_refuses_what_is_not_on_the_gpu(G):
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError, match="device"):
+        G.page_tables(i(2), i(2), i(9), i(1), i(2, 4), 16, 3)
+    pages = torch.zeros((3, 2, 16, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="device"):
+        G.cache_append(pages[0], pages[0], i(16), pages, pages)
+    with pytest.raises(ValueError, match="device"):
+        G.paged_attention(torch.zeros((2, 1, 64), dtype=torch.bfloat16), pages, pages, i(1, 2), i(1))
+
+
+def test_binding_refuses_numbers_out_of_range(G):
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    pages = torch.zeros((3, 2, 16, 64), dtype=torch.bfloat16)
+    q = torch.zeros((2, 1, 64), dtype=torch.bfloat16)
+    for kw in (dict(anchor=-1), dict(window=-1), dict(window=2 ** 32), dict(anchor=2 ** 31)):
+        with pytest.raises(ValueError, match=next(iter(kw))):
+            G.paged_attention(q, pages, pages, i(1, 2), i(1), **kw)
+    for size, tokens in ((0, 1), (2 ** 32 + 16, 1), (16, -1), (16, 2 ** 32)):
+        with pytest.raises(ValueError, match="must be in"):
+            G.page_tables(i(2), i(2), i(9), i(1), i(2, 4), size, tokens)
+
+
+def test_binding_refuses_a_library_without_the_calls(G, monkeypatch):
+    from paper_2607_03612_amd import binding
+
+    monkeypatch.setattr(G, "_LIB", None)
+    monkeypatch.setattr(binding, "_LIB", ctypes.CDLL(None))
+    with pytest.raises(AttributeError, match="saf3r_page"):
+        G._lib()
+
+
+# ------------------------------------------------------------- sanitizers
+
+
+def test_host_layer_is_clean_under_sanitizers(tmp_path):
+    gxx = shutil.which("g++")
+    if not gxx:
+        pytest.skip("g++ not available")
+    out = str(tmp_path / "libsaf3r_asan.so")
+    csrc = os.path.join(ROOT, "paper_2607_03612_amd", "csrc")
+    cmd = [gxx, "-std=c++17", "-g", "-O1", "-fPIC", "-shared", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+           "-fno-omit-frame-pointer", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", os.path.join(ROOT, "include"),
+           os.path.join(csrc, "api.cpp"), os.path.join(csrc, "paged_api.cpp"),
+           os.path.join(ROOT, "tests", "sanitize", "launch_stubs.cpp"),
+           os.path.join(ROOT, "tests", "sanitize", "paged_stubs.cpp"), "-o", out]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+    asan = subprocess.run([gxx, "-print-file-name=libasan.so"], capture_output=True, text=True).stdout.strip()
+    env = dict(os.environ, LD_PRELOAD=asan, ASAN_OPTIONS="detect_leaks=0:abort_on_error=1:halt_on_error=1",
+               UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1", SAF3R_LIBRARY=out, PYTHONPATH=ROOT)
+    res = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-p", "no:cacheprovider",
+                          "tests/test_paged_abi_cpu.py", "tests/sanitize/paged_paths.py"], cwd=ROOT, env=env,
+                         capture_output=True, text=True, timeout=600)
+    report = res.stdout[-4000:] + res.stderr[-4000:]
+    assert res.returncode == 0, report
+    assert "ERROR: AddressSanitizer" not in report and "runtime error" not in report, report
+    assert " passed" in res.stdout
+
+
+# --------------------------------------------------------- compiled kernels
+
+
+def test_kernels_use_no_scratch_and_no_packed_fp32(tmp_path):
+    from paper_2607_03612_amd import build
+
+    for source in ("paged.hip", "paged_attn.hip"):
+        text = open(build.device_asm(source, str(tmp_path / (source + ".s")))).read()
+        assert "scratch_" not in text and not re.search(r"v_pk_(add|mul|fma)_f32", text), source
+        sizes = [int(x) for x in re.findall(r"\.private_segment_fixed_size:\s+(\d+)", text)]
+        spills = [int(x) for x in re.findall(r"\.vgpr_spill_count:\s+(\d+)", text)]
+        assert sizes and not any(sizes) and not any(spills), source
+
+
+# ----------------------------------------------------- the plain definition
+
+
+def test_definition_of_a_step_by_hand():
+    # pages of 16; the stack's top is its end: 7, 5, 9
+    got = O.page_tables([16, 20, 0, 5], [1, -1, 17, 2], [9, 5, 7] + [0] * 7, 3, [[1, -1], [2, 3], [-1, -1], [4, -1]], 16, 24)
+    assert list(got["free"][:5]) == [9, 5, 7, 2, 3]  # the ended sequence's pages, its first one first
+    # request 0 takes page 3, request 2 takes 2 and 7; request 3 has room
+    assert got["table"].tolist() == [[1, 3], [2, 3], [2, 7], [4, -1]] and got["count"] == 2
+    assert list(got["lengths"]) == [17, 0, 17, 7] and list(got["start"]) == [0, 1, 1, 18, 20]
+    assert list(got["slots"]) == [48] + list(range(32, 48)) + [112] + [69, 70] + [-1] * 4
+
+
+def test_definition_refuses_by_hand():
+    # two pages left: request 0 wants three, so request 2 gets none either, request 1 needs none
+    got = O.page_tables([0, 3, 0], [40, 4, 1], [5, 6] + [0] * 5, 2, [[-1] * 3, [1, -1, -1], [-1] * 3], 16, 99)
+    assert list(got["lengths"]) == [0, 7, 0] and got["count"] == 2 and list(got["start"]) == [0, 40, 44, 45]
+    assert list(got["slots"][:40]) == [-1] * 40 and list(got["slots"][40:45]) == [19, 20, 21, 22, -1]
+
+
+def test_definition_of_8_bit_values():
+    values = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    np.testing.assert_array_equal(O.e4m3_values(), values)
+    x = np.concatenate([np.random.default_rng(0).uniform(-448, 448, 5000), np.linspace(-2.0 ** -5, 2.0 ** -5, 4001),
+                        (values[:126] + values[1:127]) / 2, -(values[:126] + values[1:127]) / 2, values[:127]])
+    want = torch.from_numpy(x.astype(np.float32)).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    np.testing.assert_array_equal(O.to_e4m3(x.astype(np.float32).astype(np.float64)), want)
+
+
+def test_definition_of_8_bit_rows():
+    for scale in (1e-30, 1e-3, 1.0, 448.0, 1e30):
+        x = torch.randn((50, 64), generator=torch.Generator().manual_seed(1)).mul(scale).bfloat16().double().numpy()
+        codes, e = O.quantise(x)
+        p = e.astype(float) - 127
+        largest = np.abs(x).max(1)
+        assert np.all(largest <= 448 * 2.0 ** p) and np.all((largest > 448 * 2.0 ** (p - 1)) | (e == 1))
+        back = O.e4m3_values()[codes] * 2.0 ** p[:, None]
+        # half a step of the value, or of the smallest e4m3 numbers
+        assert np.all(np.abs(back - x) <= np.maximum(2.0 ** -4 * np.abs(x), 2.0 ** -10 * 2.0 ** p[:, None]))
+    codes, e = O.quantise(np.zeros((2, 64)))
+    assert not codes.any() and list(e) == [1, 1]
+
+
+def test_definition_of_attention():
+    rng = np.random.default_rng(2)
+    q, k, v = rng.standard_normal((6, 64)), rng.standard_normal((37, 2, 64)), rng.standard_normal((37, 2, 64))
+    out, lse, size, terms = O.attend(q, k, v, 0.3)
+    tq = torch.from_numpy(q)[:, None]
+    tk, tv = (torch.from_numpy(x).transpose(0, 1).repeat_interleave(3, 0) for x in (k, v))
+    want = torch.nn.functional.scaled_dot_product_attention(tq, tk, tv, scale=0.3)[:, 0]
+    np.testing.assert_allclose(out, want.numpy(), rtol=1e-12, atol=1e-13)
+    z = 0.3 * (tq @ tk.transpose(1, 2))[:, 0]
+    np.testing.assert_allclose(lse, torch.logsumexp(z, 1).numpy(), rtol=1e-13)
+    assert np.all(size >= np.abs(z.numpy()).max(1)) and np.all(terms >= np.abs(out))
+    empty = O.attend(q, k[:0], v[:0], 0.3)
+    assert not empty[0].any() and np.all(empty[1] == -np.inf)
+    assert list(O.kept_tokens(6, 1, 2)) == [0, 4, 5] and list(O.kept_tokens(3, 2, 2)) == [0, 1, 2] and len(O.kept_tokens(0, 3, 1)) == 0
