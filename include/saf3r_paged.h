@@ -23,6 +23,8 @@
  * workspaces do not overlap. A workspace is overwritten and holds nothing
  * between calls; calls that share one must be ordered on the GPU.
  *
+ * Strides count elements; a stride along a dimension of one entry is not looked at.
+ *
  * What the GPU reads from lengths, tables and slots is bounded there: a bad
  * entry gives no access outside the arrays, as each call says.
  *
@@ -34,7 +36,7 @@
  *   SAF3R_CACHE_BF16  bf16, with bf16 ones;
  *   SAF3R_CACHE_E4M3  8-bit OCP e4m3, with bf16 tokens, queries and outputs, and
  *                     one power of two per token and head: the value is
- *                     code * 2^(exp - 127), exp a uint8 in
+ *                     code * 2^(exp - 127), exp a uint8 of 1 .. 254 in
  *                     [pages][kv_heads][page_size] (contiguous, one array for K
  *                     and one for V).
  */
@@ -56,7 +58,7 @@ typedef struct {
   int32_t head_dim;     /* 64 or 128 */
   int32_t dtype;        /* saf3r_cache_dtype */
   int32_t reserved;     /* 0 */
-  int64_t page_stride;  /* elements; every stride >= 0 and a multiple of 16 bytes, */
+  int64_t page_stride;  /* every stride >= 0 and a multiple of 16 bytes, */
   int64_t head_stride;  /*   page_size * token_stride under 2^30 bytes */
   int64_t token_stride;
 } saf3r_page_layout;
@@ -131,7 +133,7 @@ saf3r_status saf3r_page_tables(const saf3r_page_step* step, const int32_t* lengt
  *   slots          int32 [tokens]
  *   k_pages, v_pages  16-byte aligned
  *   k_exp, v_exp   the exponents of an E4M3 cache (4-byte aligned), else NULL
- * tokens 0 .. 2^30; none is not an error. */
+ * tokens 0 .. 2^26; none is not an error. */
 typedef struct {
   int32_t tokens;
   int32_t reserved; /* 0 */

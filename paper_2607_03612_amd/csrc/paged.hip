@@ -9,27 +9,48 @@ constexpr int kSlotThreads = 256;
 // of additions does not matter.
 __device__ inline uint32_t add_to(uint32_t a, uint32_t b, uint32_t limit) { return min(a + b, limit); }
 
-// Sums of the threads before this one; `total` gets the sum of all.
-template <int kScanThreads>
-__device__ inline uint32_t scan(uint32_t x, uint32_t limit, uint32_t* waves, uint32_t& total) {
+// The sum over a wave's lanes up to and with this one: within rows of 16 lanes, then
+// each row's last lane to the rows behind it, all in registers.
+template <int kCtrl, int kRows>
+__device__ inline uint32_t shifted(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, kRows, 0xf, false);
+}
+__device__ inline uint32_t wave_scan(uint32_t x, uint32_t limit) {
+  x = add_to(x, shifted<0x111, 0xf>(x), limit);  // from 1, 2, 4, 8 lanes before
+  x = add_to(x, shifted<0x112, 0xf>(x), limit);
+  x = add_to(x, shifted<0x114, 0xf>(x), limit);
+  x = add_to(x, shifted<0x118, 0xf>(x), limit);
+  x = add_to(x, shifted<0x142, 0xa>(x), limit);  // lane 15 to row 1, 47 to row 3
+  x = add_to(x, shifted<0x143, 0xc>(x), limit);  // lane 31 to rows 2 and 3
+  return x;
+}
+
+// Sums of the threads before this one, for kSums values at once; `total` gets those
+// of all.
+template <int kThreads, int kSums>
+__device__ inline void scan(const uint32_t (&x)[kSums], const uint32_t (&limit)[kSums], uint32_t (*waves)[kThreads / 64],
+                            uint32_t (&before)[kSums], uint32_t (&total)[kSums]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t to[kSums];
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t y = __shfl_up(x, d);
-    if (lane >= d) x = add_to(x, y, limit);
-  }
+  for (int i = 0; i < kSums; ++i) to[i] = wave_scan(x[i], limit[i]);
   __syncthreads();  // the last scan's reads of `waves`
-  if (lane == 63) waves[wave] = x;
-  __syncthreads();
-  uint32_t before = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kScanThreads / 64; ++w) {
-    if (w == wave) before = all;
-    all = add_to(all, waves[w], limit);
+  for (int i = 0; i < kSums; ++i)
+    if (lane == 63) waves[i][wave] = to[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSums; ++i) {
+    uint32_t ahead = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) {
+      if (w == wave) ahead = all;
+      all = add_to(all, waves[i][w], limit[i]);
+    }
+    total[i] = all;
+    const uint32_t y = __shfl_up(to[i], 1);
+    before[i] = lane == 0 ? ahead : add_to(ahead, y, limit[i]);
   }
-  total = all;
-  const uint32_t y = __shfl_up(x, 1);
-  return lane == 0 ? before : add_to(before, y, limit);
 }
 
 // The last of `n` ascending entries, the first of which is at most x, that is.
@@ -74,10 +95,16 @@ struct Request {
   uint32_t back, behind;  // pages it gives back, and those of the requests before it
 };
 
+// Sums over the requests so far.
+struct Sums {
+  uint32_t tokens, back;  // of the first pass: new tokens, pages given back
+  uint32_t need;          // of the second: pages asked for
+};
+
 template <int kThreads>
 __device__ inline Request read_request(int r, const int32_t* lengths, const int32_t* __restrict__ new_tokens, const StepArgs& a,
-                                       uint32_t* waves, uint32_t& tokens_before, uint32_t& back_before) {
-  const uint32_t token_limit = (uint32_t)a.tokens + 1, page_limit = (uint32_t)a.pages + 1;
+                                       uint32_t (*waves)[kThreads / 64], Sums& sums) {
+  const uint32_t limit[2] = {(uint32_t)a.tokens + 1, (uint32_t)a.pages + 1};
   const int32_t capacity = a.max_pages * a.page.size;
   int32_t length = -1, fresh = 0;
   if (r < a.requests) {
@@ -87,17 +114,90 @@ __device__ inline Request read_request(int r, const int32_t* lengths, const int3
   const bool good = length >= 0 && length <= capacity;
   const bool ends = good && fresh < 0;
   const int32_t held = good ? div_page(a.page, length + a.page.size - 1) : 0;
-  const uint32_t grow = min((uint32_t)max(fresh, 0), token_limit);
+  const uint32_t x[2] = {min((uint32_t)max(fresh, 0), limit[0]), ends ? min((uint32_t)held, limit[1]) : 0};
+  uint32_t before[2], total[2];
+  scan<kThreads, 2>(x, limit, waves, before, total);
   Request q;
-  uint32_t total;
-  q.first = add_to(tokens_before, scan<kThreads>(grow, token_limit, waves, total), token_limit);
-  tokens_before = add_to(tokens_before, total, token_limit);
-  q.back = ends ? min((uint32_t)held, page_limit) : 0;
-  q.behind = add_to(back_before, scan<kThreads>(q.back, page_limit, waves, total), page_limit);
-  back_before = add_to(back_before, total, page_limit);
-  q.rec = RequestRecord{length, good && !ends && q.first + grow < token_limit ? 0 : -1, held};
+  q.first = add_to(sums.tokens, before[0], limit[0]);
+  sums.tokens = add_to(sums.tokens, total[0], limit[0]);
+  q.back = x[1];
+  q.behind = add_to(sums.back, before[1], limit[1]);
+  sums.back = add_to(sums.back, total[1], limit[1]);
+  q.rec = RequestRecord{length, good && !ends && q.first + x[0] < limit[0] ? 0 : -1, held};
   q.fresh = fresh;
   return q;
+}
+
+// The second pass: the pages that a request takes, and its length after the step. The
+// sums grow with r, so the pages taken in all are the last sum that fits.
+template <int kThreads>
+__device__ inline int32_t take_pages(RequestRecord& rec, int32_t fresh, uint32_t top, const StepArgs& a,
+                                     uint32_t (*waves)[kThreads / 64], Sums& sums, uint32_t* taken) {
+  const uint32_t limit[1] = {(uint32_t)a.pages + 1};
+  const int32_t capacity = a.max_pages * a.page.size;
+  const bool ends = fresh < 0 && rec.length >= 0 && rec.length <= capacity;
+  const bool may = rec.top == 0 && fresh <= capacity - rec.length;
+  const int32_t after = may ? rec.length + fresh : 0;
+  const uint32_t need[1] = {may ? min((uint32_t)(div_page(a.page, after + a.page.size - 1) - rec.held), limit[0]) : 0};
+  uint32_t before[1], total[1];
+  scan<kThreads, 1>(need, limit, waves, before, total);
+  const uint32_t first = add_to(sums.need, before[0], limit[0]), to = add_to(first, need[0], limit[0]);
+  sums.need = add_to(sums.need, total[0], limit[0]);
+  const bool fits = may && (need[0] == 0 || to <= top);
+  rec.top = !fits ? -1 : need[0] == 0 ? 0 : (int32_t)(top - 1 - first);
+  const uint64_t some = __ballot(fits && need[0] > 0);
+  if (some && (threadIdx.x & 63) == 63 - __clzll((long long)some)) atomicMax(taken, to);
+  return ends ? 0 : fits ? after : rec.length;
+}
+
+// A step of up to kThreads requests. The order of the requests is the order of the
+// threads: ended sequences' pages are counted first, since what they give back
+// decides who fits, then the pages that the others need. Every workgroup does this
+// for itself and then finds the slots of its share of the new tokens and copies its
+// share of the pages given back; the first one writes what belongs to the requests. No
+// workgroup waits for another: a page that an ended sequence gave back is read from
+// that sequence's row, not from the stack. (Two launches, one to count and one with a
+// thread per token: 10.2 us for 1000 requests at 1024 to 16384 tokens where this takes
+// 5.2, and 4 us more of the host's time.)
+template <int kThreads>
+__global__ __launch_bounds__(kThreads) void page_step_kernel(
+    const int32_t* lengths, const int32_t* __restrict__ new_tokens, int32_t* free_pages, const int32_t* free_count,
+    int32_t* table, int32_t* lengths_out, int32_t* count_out, int32_t* __restrict__ start_out,
+    int32_t* __restrict__ slots, StepArgs a) {
+  __shared__ uint32_t waves[2][kThreads / 64];
+  __shared__ uint32_t starts[kThreads];
+  __shared__ uint32_t behind[kThreads];
+  __shared__ RequestRecord records[kThreads];
+  __shared__ uint32_t taken;
+  const int r = threadIdx.x;
+  if (r == 0) taken = 0;
+  const uint32_t count = (uint32_t)min(max(*free_count, 0), a.pages);
+  Sums sums{0, 0, 0};
+  Request q = read_request<kThreads>(r, lengths, new_tokens, a, waves, sums);
+  starts[r] = min(q.first, (uint32_t)a.tokens);
+  behind[r] = q.behind;
+  const int32_t end = (int32_t)min(sums.tokens, (uint32_t)a.tokens);
+  const uint32_t top = min(count + sums.back, (uint32_t)a.pages);
+  const int32_t after = take_pages<kThreads>(q.rec, q.fresh, top, a, waves, sums, &taken);
+  records[r] = q.rec;
+  if (blockIdx.x == 0 && r < a.requests) {
+    start_out[r] = (int32_t)starts[r];
+    lengths_out[r] = after;
+  }
+  __syncthreads();
+  if (blockIdx.x == 0 && r == 0) {
+    start_out[a.requests] = end;
+    *count_out = (int32_t)(top - taken);
+  }
+  const auto given_back = [&](uint32_t i) {
+    const int from = last_up_to(behind, a.requests, i);
+    return table[(int64_t)from * a.max_pages + (i - behind[from])];
+  };
+  const auto stack = [&](int32_t i) { return (uint32_t)i < count ? free_pages[i] : given_back((uint32_t)i - count); };
+  const uint32_t mine = blockIdx.x * kThreads + r, all = gridDim.x * kThreads;
+  for (uint32_t t = mine; t < (uint32_t)a.tokens; t += all)
+    slots[t] = (int32_t)t < end ? slot_of((int32_t)t, starts, records, stack, table, a) : -1;
+  for (uint32_t i = mine; i < top - count; i += all) free_pages[count + i] = given_back(i);
 }
 
 // A wave copies its ended requests' rows to the stack one after another; a sum at
@@ -116,88 +216,6 @@ __device__ inline void push_pages(int r, const Request& q, uint32_t count, int32
   }
 }
 
-// The second pass: the pages that a request takes, and its length after the step.
-template <int kThreads>
-__device__ inline int32_t take_pages(RequestRecord& rec, int32_t fresh, uint32_t top, const StepArgs& a, uint32_t* waves,
-                                     uint32_t& need_before, uint32_t& taken) {
-  const uint32_t page_limit = (uint32_t)a.pages + 1;
-  const int32_t capacity = a.max_pages * a.page.size;
-  const bool ends = fresh < 0 && rec.length >= 0 && rec.length <= capacity;
-  const bool may = rec.top == 0 && fresh <= capacity - rec.length;
-  const int32_t after = may ? rec.length + fresh : 0;
-  const uint32_t need = may ? min((uint32_t)(div_page(a.page, after + a.page.size - 1) - rec.held), page_limit) : 0;
-  uint32_t total;
-  const uint32_t first = add_to(need_before, scan<kThreads>(need, page_limit, waves, total), page_limit);
-  const uint32_t to = add_to(first, need, page_limit);
-  need_before = add_to(need_before, total, page_limit);
-  const bool fits = may && (need == 0 || to <= top);
-  rec.top = !fits ? -1 : need == 0 ? 0 : (int32_t)(top - 1 - first);
-  // the sums grow with r, so the pages taken are the last sum that fits
-  uint32_t mine = fits && need > 0 ? to : 0;
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) mine = max(mine, (uint32_t)__shfl_xor((int)mine, d));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = mine;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) taken = max(taken, waves[w]);
-  return ends ? 0 : fits ? after : rec.length;
-}
-
-// A step of up to kThreads requests. The order of the requests is the order of the
-// threads: ended sequences' pages are counted first, since what they give back
-// decides who fits, then the pages that the others need. Every workgroup does this
-// for itself and then finds the slots of its own new tokens; the first one writes
-// what belongs to the requests. No workgroup waits for another: a page that an ended
-// sequence gave back is read from that sequence's row, not from the stack. (Two
-// launches, one to count and one with a thread per token: 10.2 us for 1000 requests
-// at 4096 to 16384 tokens, and 4 us more of the host's time.)
-template <int kThreads>
-__global__ __launch_bounds__(kThreads) void page_step_kernel(
-    const int32_t* lengths, const int32_t* __restrict__ new_tokens, int32_t* free_pages, const int32_t* free_count,
-    int32_t* table, int32_t* lengths_out, int32_t* count_out, int32_t* __restrict__ start_out,
-    int32_t* __restrict__ slots, StepArgs a) {
-  __shared__ uint32_t waves[kThreads / 64];
-  __shared__ uint32_t starts[kThreads];
-  __shared__ uint32_t behind[kThreads];
-  __shared__ RequestRecord records[kThreads];
-  const int r = threadIdx.x;
-  const uint32_t count = (uint32_t)min(max(*free_count, 0), a.pages);
-  uint32_t tokens = 0, back = 0;
-  Request q = read_request<kThreads>(r, lengths, new_tokens, a, waves, tokens, back);
-  starts[r] = min(q.first, (uint32_t)a.tokens);
-  behind[r] = q.behind;
-  const int32_t end = (int32_t)min(tokens, (uint32_t)a.tokens);
-  const uint32_t top = min(count + back, (uint32_t)a.pages);
-  uint32_t need = 0, taken = 0;
-  const int32_t after = take_pages<kThreads>(q.rec, q.fresh, top, a, waves, need, taken);
-  records[r] = q.rec;
-  if (blockIdx.x == 0) {
-    if (r < a.requests) {
-      start_out[r] = (int32_t)starts[r];
-      lengths_out[r] = after;
-    }
-    if (r == 0) {
-      start_out[a.requests] = end;
-      *count_out = (int32_t)(top - taken);
-    }
-    push_pages(r, q, count, free_pages, table, a);
-  }
-  __syncthreads();
-  const auto stack = [&](int32_t i) {
-    if ((uint32_t)i < count) return free_pages[i];
-    const uint32_t off = (uint32_t)i - count;
-    const int from = last_up_to(behind, a.requests, off);
-    return table[(int64_t)from * a.max_pages + (off - behind[from])];
-  };
-  const int32_t first = (int32_t)blockIdx.x * (kThreads * kSlotsEach);
-#pragma unroll
-  for (int i = 0; i < kSlotsEach; ++i) {
-    const int32_t t = first + i * kThreads + r;
-    if (t < a.tokens) slots[t] = t < end ? slot_of(t, starts, records, stack, table, a) : -1;
-  }
-}
-
 // A step of any number of requests, kScanThreads a turn, by one workgroup; the slots
 // follow in a launch of their own.
 constexpr int kScanThreads = 1024;
@@ -205,20 +223,21 @@ __global__ __launch_bounds__(kScanThreads) void page_scan_kernel(
     const int32_t* lengths, const int32_t* __restrict__ new_tokens, int32_t* free_pages,
     const int32_t* free_count, const int32_t* table, int32_t* lengths_out, int32_t* count_out,
     int32_t* __restrict__ start_out, RequestRecord* __restrict__ records, StepArgs a) {
-  __shared__ uint32_t waves[kScanThreads / 64];
+  __shared__ uint32_t waves[2][kScanThreads / 64];
+  __shared__ uint32_t taken;
+  if (threadIdx.x == 0) taken = 0;
   const uint32_t count = (uint32_t)min(max(*free_count, 0), a.pages);
-  uint32_t tokens = 0, back = 0;
+  Sums sums{0, 0, 0};
   for (int r0 = 0; r0 < a.requests; r0 += kScanThreads) {
     const int r = r0 + threadIdx.x;
-    const Request q = read_request<kScanThreads>(r, lengths, new_tokens, a, waves, tokens, back);
+    const Request q = read_request<kScanThreads>(r, lengths, new_tokens, a, waves, sums);
     if (r < a.requests) {
       start_out[r] = (int32_t)min(q.first, (uint32_t)a.tokens);
       records[r] = q.rec;
     }
     push_pages(r, q, count, free_pages, table, a);
   }
-  const uint32_t top = min(count + back, (uint32_t)a.pages);
-  uint32_t need = 0, taken = 0;
+  const uint32_t top = min(count + sums.back, (uint32_t)a.pages);
   for (int r0 = 0; r0 < a.requests; r0 += kScanThreads) {
     const int r = r0 + threadIdx.x;
     RequestRecord rec{-1, -1, 0};
@@ -227,14 +246,15 @@ __global__ __launch_bounds__(kScanThreads) void page_scan_kernel(
       rec = records[r];
       fresh = new_tokens[r];
     }
-    const int32_t after = take_pages<kScanThreads>(rec, fresh, top, a, waves, need, taken);
+    const int32_t after = take_pages<kScanThreads>(rec, fresh, top, a, waves, sums, &taken);
     if (r < a.requests) {
       records[r].top = rec.top;
       lengths_out[r] = after;
     }
   }
+  __syncthreads();
   if (threadIdx.x == 0) {
-    start_out[a.requests] = (int32_t)min(tokens, (uint32_t)a.tokens);
+    start_out[a.requests] = (int32_t)min(sums.tokens, (uint32_t)a.tokens);
     *count_out = (int32_t)(top - taken);
   }
 }
@@ -333,10 +353,12 @@ hipError_t launch_page_tables(const int32_t* lengths, const int32_t* new_tokens,
                               int32_t* count_out, int32_t* start, int32_t* slots,
                               RequestRecord* records, const StepArgs& a, hipStream_t s) {
   if (page_tables_in_one(a.requests, a.tokens, a.in_place != 0)) {
-    // four waves where they are enough (64 requests, 1024 tokens: 5.7 us, 6.6 with 16)
-    const bool small = a.requests <= 256 && a.tokens <= 256 * kSlotsEach;
-    const int each = (small ? 256 : kStepRequests) * kSlotsEach;
-    const dim3 grid((unsigned)(a.tokens > each ? (a.tokens + each - 1) / each : 1));
+    // four waves where they are as many as the requests ask for; in place, one
+    // workgroup and more of them for many tokens
+    const bool small = a.requests <= 256 && (!a.in_place || a.tokens <= 1024);
+    const int threads = small ? 256 : kStepRequests;
+    const int64_t want = ((int64_t)a.tokens + threads - 1) / threads;
+    const dim3 grid(a.in_place || want < 1 ? 1u : (unsigned)(want < kStepGroups ? want : kStepGroups));
     if (small)
       hipLaunchKernelGGL(page_step_kernel<256>, grid, dim3(256), 0, s, lengths, new_tokens, free_pages, free_count, table,
                          lengths_out, count_out, start, slots, a);

@@ -18,8 +18,10 @@ saf3r_status check_page_size(int32_t page_size) {
   return SAF3R_OK;
 }
 
-// A stride of `size`-byte elements as bytes, in [0, limit]; -1 if it is none.
-int64_t stride_bytes(int64_t stride, int size, int64_t limit) {
+// A stride of `size`-byte elements along `n` entries as bytes, in [0, limit]; -1 if it
+// is none. Along one entry it says nothing and is 0.
+int64_t stride_bytes(int64_t stride, int64_t n, int size, int64_t limit) {
+  if (n == 1) return 0;
   if (stride < 0 || stride > limit / size || stride * size % 16 != 0) return -1;
   return stride * size;
 }
@@ -39,9 +41,9 @@ saf3r_status check_cache(const saf3r_page_layout* c, Cache* out) {
   if (c->kv_heads > saf3r::kMaxPagedHeads) return SAF3R_ERR_UNSUPPORTED;
   if ((int64_t)c->pages * c->page_size > INT32_MAX) return SAF3R_ERR_UNSUPPORTED;
   out->size = c->dtype == SAF3R_CACHE_F32 ? 4 : c->dtype == SAF3R_CACHE_BF16 ? 2 : 1;
-  out->page = stride_bytes(c->page_stride, out->size, kMaxStride >> 13);  // times up to 2^27 pages
-  out->head = stride_bytes(c->head_stride, out->size, kMaxStride);
-  out->token = stride_bytes(c->token_stride, out->size, (((int64_t)1 << 30) - 1) / c->page_size);
+  out->page = stride_bytes(c->page_stride, c->pages, out->size, kMaxStride >> 13);  // times up to 2^27 pages
+  out->head = stride_bytes(c->head_stride, c->kv_heads, out->size, kMaxStride);
+  out->token = stride_bytes(c->token_stride, c->page_size, out->size, (((int64_t)1 << 30) - 1) / c->page_size);
   if (out->page < 0 || out->head < 0 || out->token < 0) return SAF3R_ERR_INVALID_ARGUMENT;
   return SAF3R_OK;
 }
@@ -69,8 +71,12 @@ saf3r_status check_decode(const saf3r_page_layout* cache, const saf3r_decode* d,
     return SAF3R_ERR_UNSUPPORTED;
   const int wide = cache->dtype == SAF3R_CACHE_F32 ? 4 : 2;
   const int64_t strides[4] = {d->q_head_stride, d->q_request_stride, d->out_head_stride, d->out_request_stride};
-  for (int64_t s : strides)
-    if (stride_bytes(s, wide, kMaxStride) < 0) return SAF3R_ERR_INVALID_ARGUMENT;
+  int64_t* to[4] = {&a->q_head, &a->q_request, &a->out_head, &a->out_request};
+  for (int i = 0; i < 4; ++i) {
+    const int64_t bytes = stride_bytes(strides[i], i % 2 == 0 ? d->q_heads : d->requests, wide, kMaxStride);
+    if (bytes < 0) return SAF3R_ERR_INVALID_ARGUMENT;
+    *to[i] = bytes / wide;
+  }
   a->requests = d->requests;
   a->q_heads = d->q_heads;
   a->kv_heads = cache->kv_heads;
@@ -85,10 +91,6 @@ saf3r_status check_decode(const saf3r_page_layout* cache, const saf3r_decode* d,
   a->token_stride = (int32_t)c->token;
   a->page_stride = c->page;
   a->head_stride = c->head;
-  a->q_head = d->q_head_stride;
-  a->q_request = d->q_request_stride;
-  a->out_head = d->out_head_stride;
-  a->out_request = d->out_request_stride;
   return SAF3R_OK;
 }
 
@@ -146,11 +148,11 @@ saf3r_status saf3r_cache_append(const saf3r_page_layout* cache, const saf3r_toke
   const saf3r_status st = check_cache(cache, &c);
   if (st != SAF3R_OK) return st;
   if (!rows || rows->tokens < 0 || rows->reserved != 0) return SAF3R_ERR_INVALID_ARGUMENT;
-  if (rows->tokens > saf3r::kMaxStepTokens) return SAF3R_ERR_UNSUPPORTED;
+  if (rows->tokens > saf3r::kMaxAppendTokens) return SAF3R_ERR_UNSUPPORTED;
   const int wide = cache->dtype == SAF3R_CACHE_F32 ? 4 : 2;
   saf3r::AppendArgs a{};
-  a.row_head = stride_bytes(rows->head_stride, wide, kMaxStride);
-  a.row_token = stride_bytes(rows->token_stride, wide, kMaxStride >> 12);
+  a.row_head = stride_bytes(rows->head_stride, cache->kv_heads, wide, kMaxStride);
+  a.row_token = stride_bytes(rows->token_stride, rows->tokens, wide, kMaxStride >> 12);
   if (a.row_head < 0 || a.row_token < 0) return SAF3R_ERR_INVALID_ARGUMENT;
   if (!k_pages || !v_pages || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !exps_ok(cache->dtype, k_exp, v_exp))
     return SAF3R_ERR_INVALID_ARGUMENT;

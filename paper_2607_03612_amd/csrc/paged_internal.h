@@ -12,6 +12,10 @@ constexpr int kMaxPagedHeads = 256;
 constexpr int kMaxRequests = 65536;
 constexpr int64_t kMaxRowTokens = (int64_t)1 << 29;  // of a request: max_pages * page_size
 constexpr int64_t kMaxStepTokens = (int64_t)1 << 30;
+// A launch's threads in one dimension stay under 2^32: of append_kernel 32 a token,
+// of paged_rows_kernel 512 a row.
+constexpr int64_t kMaxAppendTokens = (int64_t)1 << 26;
+constexpr int64_t kMaxWholeRows = (int64_t)1 << 22;
 
 // x / page_size for 0 <= x < 2^29 + kMaxPageSize, as one high product: with d =
 // page_size / 16 <= 64 and m = ceil(2^31 / d), floor(x / 16) * (m d - 2^31) < 2^31.
@@ -45,13 +49,14 @@ struct RequestRecord {
   int32_t held;    // pages before the step
 };
 
-// Steps of up to so many requests are one launch, without a workspace, of as many
-// workgroups as it takes to give each thread kSlotsEach new tokens. In place the
-// workgroups would read what the first one writes, so there only of one.
+// Steps of up to so many requests are one launch, without a workspace, of up to so many
+// workgroups, a token a thread if that is enough. In place the workgroups would read
+// what the first one writes, so there it is one, for steps of few tokens.
 constexpr int kStepRequests = 1024;
-constexpr int kSlotsEach = 4;
+constexpr int kStepGroups = 512;
+constexpr int kStepInPlaceTokens = 4096;
 inline bool page_tables_in_one(int32_t requests, int32_t tokens, bool in_place) {
-  return requests <= kStepRequests && (!in_place || tokens <= kStepRequests * kSlotsEach);
+  return requests <= kStepRequests && (!in_place || tokens <= kStepInPlaceTokens);
 }
 hipError_t launch_page_tables(const int32_t* lengths, const int32_t* new_tokens, int32_t* free_pages,
                               const int32_t* free_count, int32_t* table, int32_t* lengths_out,
@@ -92,14 +97,12 @@ struct DecodeArgs {
   int64_t q_head, q_request, out_head, out_request;
 };
 
-// Shared-out launches: 512 workgroups of four waves, two waves to a SIMD. Each wave
-// takes the same number of tiles, at least kMinTiles, so that a short launch does
-// not spend itself on joining.
+// Shared-out launches: 512 workgroups of four waves, two waves to a SIMD (with 1024
+// 5 to 20% slower where a wave has few tiles, the same elsewhere).
 constexpr int kThreads = 256;
 constexpr int kGroupWaves = kThreads / 64;
 constexpr int kWorkgroups = 512;
 constexpr int kWaves = kWorkgroups * kGroupWaves;  // a power of two
-constexpr int kMinTiles = 2;
 // Whole-row launches: eight waves share a row.
 constexpr int kRowThreads = 512;
 constexpr int kRowWaves = kRowThreads / 64;
@@ -114,7 +117,8 @@ constexpr int kRowWaves = kRowThreads / 64;
 constexpr int64_t kWholeRowBytes = 384 << 10;
 inline bool whole_rows(int dtype, int dim, const DecodeArgs& a) {
   const int size = dtype == 0 ? 4 : dtype == 1 ? 2 : 1;
-  return (int64_t)a.max_pages * a.page.size * dim * size * 2 <= kWholeRowBytes;
+  return (int64_t)a.max_pages * a.page.size * dim * size * 2 <= kWholeRowBytes &&
+         (int64_t)a.requests * a.kv_heads * a.qtiles <= kMaxWholeRows;
 }
 
 // Query heads of a row, and the workspace: an int4 per workgroup, and two parts of a

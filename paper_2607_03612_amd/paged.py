@@ -8,6 +8,7 @@ does not pass are allocated here.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 from . import binding
 from .binding import Saf3rError  # noqa: F401
@@ -178,6 +179,11 @@ def page_tables(lengths, new_tokens, free_pages, free_count, page_table, page_si
     return tuple(outs)
 
 
+def _same_strides(s, t):
+    """Whether two tensors of one shape have the same strides; along one entry they say nothing."""
+    return s.stride() == t.stride() or all(x == y or n == 1 for x, y, n in zip(s.stride(), t.stride(), s.shape))
+
+
 def _layout(k_pages, v_pages, k_exp, v_exp):
     """The pages' layout, and the type of tokens and queries beside them."""
     dtype, dev, shape, strides = k_pages.dtype, k_pages.device, k_pages.shape, k_pages.stride()
@@ -187,7 +193,7 @@ def _layout(k_pages, v_pages, k_exp, v_exp):
     _check_device(dev)
     if len(shape) != 4 or strides[3] != 1:
         raise ValueError("pages must be [pages, kv_heads, page_size, head_dim], head_dim contiguous")
-    if v_pages.shape != shape or v_pages.dtype != dtype or v_pages.device != dev or v_pages.stride() != strides:
+    if v_pages.shape != shape or v_pages.dtype != dtype or v_pages.device != dev or not _same_strides(k_pages, v_pages):
         raise ValueError("k_pages and v_pages must share shape, strides, dtype and device")
     n, H, ps, D = shape
     if code == E4M3:
@@ -221,7 +227,7 @@ def cache_append(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=N
     dev, shape, strides = k.device, k.shape, k.stride()
     if k.dtype != kind or dev != k_pages.device or len(shape) != 3 or strides[2] != 1:
         raise ValueError(f"k and v must be {kind} tensors [kv_heads, tokens, head_dim] on {k_pages.device}, head_dim contiguous")
-    if v.shape != shape or v.dtype != kind or v.device != dev or v.stride() != strides:
+    if v.shape != shape or v.dtype != kind or v.device != dev or not _same_strides(k, v):
         raise ValueError("k and v must share shape, strides, dtype and device")
     H, T, D = shape
     if H != layout.kv_heads or D != layout.head_dim:
@@ -233,11 +239,18 @@ def cache_append(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=N
           slots.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_exp), _ptr(v_exp))
 
 
+@functools.lru_cache(maxsize=256)
+def _attention_workspace(code, kv_heads, page_size, head_dim, q_heads, requests, width) -> int:
+    """The library's own answer, which these sizes alone decide."""
+    layout = PageLayout(1, page_size, kv_heads, head_dim, code, 0, 0, 0, 0)
+    step = Decode(requests, q_heads, width, 0, 0, 1.0, 0, 0, 0, 0)
+    return _lib().saf3r_paged_attention_workspace_bytes(ctypes.byref(layout), ctypes.byref(step))
+
+
 def paged_attention_workspace_bytes(q, k_pages, v_pages, page_table, k_exp=None, v_exp=None) -> int:
-    lib = _lib()
-    layout, _ = _layout(k_pages, v_pages, k_exp, v_exp)
-    step = Decode(q.shape[1], q.shape[0], page_table.shape[1], 0, 0, 1.0, 0, 0, 0, 0)
-    r = lib.saf3r_paged_attention_workspace_bytes(ctypes.byref(layout), ctypes.byref(step))
+    _lib()
+    c, _ = _layout(k_pages, v_pages, k_exp, v_exp)
+    r = _attention_workspace(c.dtype, c.kv_heads, c.page_size, c.head_dim, q.shape[0], q.shape[1], page_table.shape[1])
     binding._check(min(r, 0), "saf3r_paged_attention_workspace_bytes")
     return int(r)
 
@@ -278,7 +291,7 @@ def paged_attention(q, k_pages, v_pages, page_table, lengths, k_exp=None, v_exp=
     lse = torch.empty((Hq, R), dtype=torch.float32, device=dev) if want_lse else None
     step = Decode(R, Hq, width, anchor, window, D ** -0.5 if scale is None else scale, strides[0], strides[1], to[0], to[1])
     if workspace is None:
-        nbytes = lib.saf3r_paged_attention_workspace_bytes(ctypes.byref(layout), ctypes.byref(step))
+        nbytes = _attention_workspace(layout.dtype, layout.kv_heads, layout.page_size, D, Hq, R, width)
         binding._check(min(nbytes, 0), "saf3r_paged_attention")
         if nbytes > 0:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)

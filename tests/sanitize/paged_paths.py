@@ -56,8 +56,10 @@ def test_page_tables(requests, tokens, in_place, launches):
 @pytest.mark.parametrize("heads", [(1, 1), (256, 1), (256, 256), (96, 2)])
 def test_attention(dtype, size, dim, page, width, launches, heads):
     hq, hk = heads
+    # whole rows only while a launch's threads can be counted: 65536 requests with up to 64 rows each
+    requests = 65536 // max(1, hk // 64) // max(1, hq // hk // 16)
     layout = G.PageLayout(2097151 if page == 1024 else 9, page, hk, dim, dtype, 0, hk * page * dim, page * dim, dim)
-    step = G.Decode(65536, hq, width, 2 ** 31 - 1, 2 ** 31 - 1, 0.125, 65536 * dim, dim, dim, hq * dim)
+    step = G.Decode(requests, hq, width, 2 ** 31 - 1, 2 ** 31 - 1, 0.125, 65536 * dim, dim, dim, hq * dim)
     need = lib().saf3r_paged_attention_workspace_bytes(ctypes.byref(layout), ctypes.byref(step))
     assert need == (0 if launches == 1 else 512 * 16 + 1024 * min(hq // hk, 16) * (8 + 4 * dim))
     exps = (OK, OK) if dtype == 2 else (None, None)
@@ -66,5 +68,11 @@ def test_attention(dtype, size, dim, page, width, launches, heads):
     assert lib().saf3r_stub_paged_launches() == launches
     assert call(ctypes.byref(layout), ctypes.byref(step), OK, OK, OK, *exps, OK, OK, OK, None, None if need == 0 else OK, need,
                 None) == 0
-    rows = G.TokenLayout(1 << 30, 0, dim, 0)
+    if heads == (256, 256):
+        step.requests += 1
+        assert lib().saf3r_paged_attention_workspace_bytes(ctypes.byref(layout), ctypes.byref(step)) > 0
+        step.requests = 65536
+        assert call(ctypes.byref(layout), ctypes.byref(step), OK, OK, OK, *exps, OK, OK, OK, OK, OK, 1 << 30, None) == 0
+        assert lib().saf3r_stub_paged_launches() == 2
+    rows = G.TokenLayout(1 << 26, 0, dim, 0)
     assert lib().saf3r_cache_append(ctypes.byref(layout), ctypes.byref(rows), OK, OK, OK, OK, OK, *exps, None) == 0

@@ -31,7 +31,7 @@ hipError_t launch_page_tables(const int32_t* lengths, const int32_t* new_tokens,
             a.requests <= kMaxRequests && a.max_pages >= 1 && a.pages >= 1 && a.tokens >= 0 && a.tokens <= kMaxStepTokens &&
             (int64_t)a.max_pages * a.page.size <= kMaxRowTokens;
   // the workgroups of one launch read what the first one writes only if there is no other
-  ok = ok && (!one || a.tokens <= kStepRequests * kSlotsEach || (lengths != lengths_out && free_count != count_out));
+  ok = ok && (!one || a.tokens <= kStepInPlaceTokens || (lengths != lengths_out && free_count != count_out));
   return paged_status(ok);
 }
 
@@ -40,7 +40,7 @@ hipError_t launch_cache_append(int dtype, int dim, const void* k, const void* v,
   const bool eight = dtype == 2;
   return paged_status(dtype >= 0 && dtype <= 2 && (dim == 64 || dim == 128) && k && v && slots && k_pages && v_pages &&
                       (k_exp != nullptr) == eight && (v_exp != nullptr) == eight && page_ok(a.page) && a.tokens >= 1 &&
-                      a.heads >= 1 && a.heads <= kMaxPagedHeads && a.slots >= a.page.size && a.slots % a.page.size == 0 &&
+                      (int64_t)a.tokens * 32 < ((int64_t)1 << 32) && a.heads >= 1 && a.heads <= kMaxPagedHeads && a.slots >= a.page.size && a.slots % a.page.size == 0 &&
                       a.row_head % 16 == 0 && a.row_token % 16 == 0 && a.page_stride % 16 == 0 && a.head_stride % 16 == 0 &&
                       a.token_stride % 16 == 0 && a.page_stride >= 0 && a.row_head >= 0);
 }
@@ -55,7 +55,7 @@ hipError_t launch_paged_attention(int dtype, int dim, const void* q, const void*
   return paged_status(dtype >= 0 && dtype <= 2 && (dim == 64 || dim == 128) && q && k_pages && v_pages && table && lengths &&
                       out && (workspace || whole) && (k_exp != nullptr) == eight && (v_exp != nullptr) == eight &&
                       page_ok(a.page) && a.kv_heads >= 1 && a.group >= 1 && a.group * a.kv_heads == a.q_heads &&
-                      a.q_heads <= kMaxPagedHeads && a.qtiles == (a.group + 15) / 16 && grid <= INT32_MAX &&
+                      a.q_heads <= kMaxPagedHeads && a.qtiles == (a.group + 15) / 16 && (!whole || grid * kRowThreads < ((int64_t)1 << 32)) &&
                       (int64_t)a.max_pages * a.page.size <= kMaxRowTokens && (int64_t)a.page.size * a.token_stride < (1 << 30) &&
                       a.scale_log2 > 0 && isfinite(a.scale_log2) && a.anchor >= 0 && a.window >= 0);
 }

@@ -94,6 +94,10 @@ def test_attention_refuses(G):
                      (dict(q_heads=1), -2), (dict(max_pages=(1 << 25) + 1), -2), (dict(q_head_stride=-192), -1),
                      (dict(q_request_stride=65), -1), (dict(out_head_stride=2 ** 62), -1), (dict(out_request_stride=4), -1)):
         assert size(ctypes.byref(good), ctypes.byref(decode(G, **kw))) == want, kw
+    # along one entry a stride says nothing
+    one = layout(G, pages=1, kv_heads=1, page_stride=3, head_stride=-5)
+    assert size(ctypes.byref(one), ctypes.byref(decode(G, q_heads=1, requests=1, q_head_stride=-1, q_request_stride=7,
+                                                       out_head_stride=1, out_request_stride=2 ** 62))) > 0
     call = lib.saf3r_paged_attention
     args = [OK, OK, OK, None, None, OK, OK, OK, OK]
     names = "q k v ke ve table lengths out lse".split()
@@ -128,7 +132,7 @@ def test_append_refuses(G):
     for kw, want in BAD_LAYOUTS:
         assert run(layout(G, **kw)) == want, kw
     for rows, want in ((None, -1), ((-1, 0, 64, 64), -1), ((5, 1, 64, 64), -1), ((5, 0, -64, 64), -1), ((5, 0, 64, 60), -1),
-                       ((5, 0, 2 ** 62, 64), -1), ((5, 0, 64, 2 ** 50), -1), (((1 << 30) + 1, 0, 64, 64), -2)):
+                       ((5, 0, 2 ** 62, 64), -1), ((5, 0, 64, 2 ** 50), -1), (((1 << 26) + 1, 0, 64, 64), -2)):
         assert run(rows=rows) == want, rows
     for n in ("k", "v", "kp", "vp"):
         assert run(**{n: None}) == -1 and run(**{n: A8}) == -1, n

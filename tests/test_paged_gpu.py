@@ -402,6 +402,22 @@ def test_attention_strided_output(gpu_lib):
     assert bool((big[3] == 7).all()) and bool((big[:, 8] == 7).all()) and bool((big[:, :, 64:] == 7).all())
 
 
+def test_strides_along_one_entry_say_nothing(gpu_lib):
+    import paper_2607_03612_amd as P
+
+    c = Cache(15, "bf16", [30], 1, 64, 32)
+    q = queries(13, 2, 1, 64, "bf16")
+    want, want_lse = attend(c, q)
+    odd = [torch.as_strided(x, x.shape, (x.stride(0) if x.shape[0] > 1 else 3, 5, x.stride(2), 1)) for x in c.kv]
+    oq = torch.as_strided(q, q.shape, (q.stride(0), 7, 1))
+    out, lse = P.paged_attention(oq, odd[0], c.kv[1], c.table, c.lengths, want_lse=True,
+                                 out=torch.as_strided(torch.empty_like(q), q.shape, (64, 1, 1)))
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    k = torch.randn((1, 1, 64), device=DEV).bfloat16()
+    P.cache_append(torch.as_strided(k, k.shape, (1, 3, 1)), k, ints([40]), odd[0], odd[1])
+    assert torch.equal(c.kv[0][1, 0, 8], k[0, 0]) and torch.equal(c.kv[1][1, 0, 8], k[0, 0])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3", "f32"])
 def test_attention_far_pages(gpu_lib, dtype):
     """Pages whose bytes lie past 2^32."""
