@@ -267,9 +267,13 @@ __device__ inline void score_tile(const KeyTile<kType, kDim>& t, const uint32_t 
   for (int u = 0; u < S::kGroups; ++u) {
     z[u] = f32x4{0, 0, 0, 0};
     if constexpr (kType == 0) {
+      // four sums of a quarter of the dimensions each: shorter chains, and a quarter
+      // of the roundings that the score of a single one would go through
+      f32x4 part[4] = {z[u], z[u], z[u], z[u]};
 #pragma unroll
       for (int w = 0; w < kDim / 4; ++w)
-        z[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.w[u][w]), __uint_as_float(q[w]), z[u], 0, 0, 0);
+        part[w & 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.w[u][w]), __uint_as_float(q[w]), part[w & 3], 0, 0, 0);
+      z[u] = (part[0] + part[1]) + (part[2] + part[3]);
     } else if constexpr (kType == 1) {
 #pragma unroll
       for (int w = 0; w < kDim / 32; ++w)
