@@ -422,15 +422,14 @@ __device__ inline void load_queries(const DecodeArgs& a, const char* __restrict_
 }
 
 // Parts of rows in LDS: of each its sums and (m, l) per query.
-constexpr int kSlots = 8;
-template <int kDim>
+template <int kDim, int kSlots>
 struct Parts {
   float o[kSlots][16][kDim + 4];
   float2 ml[kSlots][16];
 };
 
-template <int kType, int kDim>
-__device__ inline void put_part(Parts<kDim>& lds, int slot, const State<kType, kDim>& st) {
+template <int kType, int kDim, int kSlots>
+__device__ inline void put_part(Parts<kDim, kSlots>& lds, int slot, const State<kType, kDim>& st) {
   using S = Shape<kType, kDim>;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const float l = across_groups_sum(st.l);
@@ -466,17 +465,12 @@ struct Sums {
 
 template <int kType, int kWidth>
 __device__ inline void put_values(const DecodeArgs& a, char* __restrict__ out, int r, int head, int d, const float* x) {
+  static_assert(kWidth == 4 || kWidth == 8, "stores of 8 or 16 bytes in bf16");
   const int64_t at = head * a.out_head + r * a.out_request + d;
   if constexpr (kType == 0) {
 #pragma unroll
-    for (int i = 0; i < kWidth; i += 2) {
-      float* to = reinterpret_cast<float*>(out) + at + i;
-      if constexpr (kWidth % 4 == 0) {
-        if (i % 4 == 0) *reinterpret_cast<f32x4*>(to) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
-      } else {
-        *reinterpret_cast<float2*>(to) = float2{x[i], x[i + 1]};
-      }
-    }
+    for (int i = 0; i < kWidth; i += 4)
+      *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + at + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
   } else {
     uint32_t w[kWidth / 2];
 #pragma unroll
@@ -484,10 +478,8 @@ __device__ inline void put_values(const DecodeArgs& a, char* __restrict__ out, i
     uint16_t* to = reinterpret_cast<uint16_t*>(out) + at;
     if constexpr (kWidth == 8)
       *reinterpret_cast<u32x4*>(to) = u32x4{w[0], w[1], w[2], w[3]};
-    else if constexpr (kWidth == 4)
-      *reinterpret_cast<u32x2*>(to) = u32x2{w[0], w[1]};
     else
-      *reinterpret_cast<uint32_t*>(to) = w[0];
+      *reinterpret_cast<u32x2*>(to) = u32x2{w[0], w[1]};
   }
 }
 
@@ -640,13 +632,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
     const int32_t* __restrict__ lengths, char* __restrict__ out, float* __restrict__ lse, void* __restrict__ workspace,
     DecodeArgs a) {
   using S = Shape<kType, kDim>;
+  constexpr int kSlots = 2 * kGroupWaves;  // a wave's first row may have begun before it, its last may go on
   __shared__ union {
     struct {
       int64_t before[kThreads];  // tiles of the requests before a thread's
       int64_t wave_sum[kGroupWaves];
       int32_t length[kThreads];  // of a thread's first request
     } deal;
-    Parts<kDim> parts;
+    Parts<kDim, kSlots> parts;
   } lds;
   __shared__ PartHead heads_of[kSlots];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -726,7 +719,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
             put_row<kType, kDim>(a, st, p, out, lse);
           } else {
             const int slot = 2 * wave + (from_start ? 1 : 0);
-            put_part<kType, kDim>(lds.parts, slot, st);
+            put_part<kType>(lds.parts, slot, st);
             if (lane == 0) heads_of[slot] = PartHead{p.r, p.first, p.heads, ends ? 1 : 0, p.s.count - 1 - p.x};
           }
         });
@@ -814,7 +807,7 @@ __global__ __launch_bounds__(kRowThreads, 2) void paged_rows_kernel(
     const uint8_t* __restrict__ k_exp, const uint8_t* __restrict__ v_exp, const int32_t* __restrict__ table,
     const int32_t* __restrict__ lengths, char* __restrict__ out, float* __restrict__ lse, DecodeArgs a) {
   using S = Shape<kType, kDim>;
-  __shared__ Parts<kDim> lds;
+  __shared__ Parts<kDim, kRowWaves> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rows = a.kv_heads * a.qtiles;
   Place<S::kGroups> next;
@@ -838,12 +831,12 @@ __global__ __launch_bounds__(kRowThreads, 2) void paged_rows_kernel(
           ++p.x;
           return false;
         },
-        [&](const State<kType, kDim>& st, const Place<S::kGroups>&, bool, bool) { put_part<kType, kDim>(lds, wave, st); });
+        [&](const State<kType, kDim>& st, const Place<S::kGroups>&, bool, bool) { put_part<kType>(lds, wave, st); });
   else
-    put_part<kType, kDim>(lds, wave, none);
+    put_part<kType>(lds, wave, none);
   __syncthreads();
   constexpr int kWidth = kDim * 16 / kRowThreads;
-  const int c = threadIdx.x >> 5, d = (threadIdx.x & 31) * kWidth;
+  const int c = threadIdx.x / (kRowThreads / 16), d = threadIdx.x % (kRowThreads / 16) * kWidth;
   if (c >= heads) return;
   Sums<kWidth> sums;
   sums.clear();

@@ -56,8 +56,8 @@ def test_page_tables(requests, tokens, in_place, launches):
 @pytest.mark.parametrize("heads", [(1, 1), (256, 1), (256, 256), (96, 2)])
 def test_attention(dtype, size, dim, page, width, launches, heads):
     hq, hk = heads
-    # whole rows only while a launch's threads can be counted: 65536 requests with up to 64 rows each
-    requests = 65536 // max(1, hk // 64) // max(1, hq // hk // 16)
+    # whole rows only while a launch's threads can be counted: 65536 requests with up to 128 rows each
+    requests = 65536 // max(1, hk // 128) // max(1, hq // hk // 16)
     layout = G.PageLayout(2097151 if page == 1024 else 9, page, hk, dim, dtype, 0, hk * page * dim, page * dim, dim)
     step = G.Decode(requests, hq, width, 2 ** 31 - 1, 2 ** 31 - 1, 0.125, 65536 * dim, dim, dim, hq * dim)
     need = lib().saf3r_paged_attention_workspace_bytes(ctypes.byref(layout), ctypes.byref(step))

@@ -576,3 +576,118 @@ def test_a_captured_step_replays(gpu_lib):
             eager, eager_lse = P.paged_attention(q, kv[0], kv[1], table, lengths, want_lse=True)
             assert torch.equal(out, eager) and torch.equal(lse, eager_lse)
     assert lengths.tolist() == [40, 40, 40] and int(count) == pages - 9
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("e4m3", 128), ("f32", 64)])
+@pytest.mark.parametrize("Hq,Hkv", [(256, 1), (256, 256), (34, 2)])
+def test_attention_many_heads(gpu_lib, dtype, D, Hq, Hkv):
+    for lengths, width in (([5, 70], None), ([5, 70, 900], 400)):  # whole rows, shared out
+        c = Cache(16, dtype, lengths, Hkv, D, 16, width=width)
+        q = queries(14, Hq, len(lengths), D, dtype)
+        out, lse = attend(c, q)
+        check_rows(c, q, out, lse, dtype)
+
+
+def test_attention_twenty_thousand_requests(gpu_lib):
+    """A thread counts 79 neighbouring requests; most hold nothing, a few are long, one has the last place."""
+    R = 20000
+    rng = np.random.default_rng(6)
+    lengths = np.where(rng.random(R) < 0.03, rng.integers(1, 40, R), 0)
+    lengths[[0, 7777, R - 1]] = 1600, 1500, 700
+    c = Cache(17, "bf16", lengths, 1, 64, 16)
+    q = queries(15, 2, R, 64, "bf16")
+    out, lse = attend(c, q)
+    some = np.flatnonzero(lengths)
+    check_rows(c, q, out, lse, "bf16", rows=[0, 7777, R - 1] + list(some[::9]))
+    none = torch.from_numpy(np.flatnonzero(lengths == 0)).to(DEV)
+    assert bool((out[:, none] == 0).all()) and bool((lse[:, none] == -math.inf).all())
+
+
+def test_page_tables_of_many_requests(gpu_lib):
+    check_tables(random_step(9, 65536, 16, 3, 60000, 20, 3000))
+    check_tables(random_step(9, 65536, 16, 3, 3000, 20, 3000), in_place=True)
+
+
+def test_a_query_that_is_none_stays_alone(gpu_lib):
+    for dtype in ("f32", "bf16", "e4m3"):
+        for lengths in ([300, 40], [3000, 40]):
+            c = Cache(18, dtype, lengths, 2, 64, 16)
+            q = queries(16, 8, 2, 64, dtype)
+            want, want_lse = attend(c, q)
+            q[3, 0, 5] = math.nan
+            out, lse = attend(c, q)
+            assert bool(out[3, 0].isnan().all()) and bool(lse[3, 0].isnan())
+            out[3, 0], lse[3, 0] = want[3, 0], want_lse[3, 0]
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+def test_two_streams_at_once(gpu_lib):
+    import paper_2607_03612_amd as P
+
+    a, b = (Cache(s, "bf16", [4000 + 500 * s, 300, 7], 2, 64, 16) for s in (19, 20))
+    qa, qb = (queries(s, 8, 3, 64, "bf16") for s in (1, 2))
+    want = [attend(a, qa), attend(b, qb)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(20):
+        for i, (c, q) in enumerate(((a, qa), (b, qb))):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(attend(c, q))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for out, lse in got[i]:
+            assert torch.equal(out, want[i][0]) and torch.equal(lse, want[i][1])
+
+
+def test_two_graphs_share_a_workspace(gpu_lib):
+    """Replayed one after the other, with eager calls on the same workspace between them."""
+    import paper_2607_03612_amd as P
+
+    caches = [Cache(21, "bf16", [5000, 60], 2, 64, 16), Cache(22, "bf16", [900, 3000, 1], 2, 64, 16)]
+    qs = [queries(3, 8, 2, 64, "bf16"), queries(4, 8, 3, 64, "bf16")]
+    need = max(P.paged_attention_workspace_bytes(q, c.kv[0], c.kv[1], c.table) for c, q in zip(caches, qs))
+    assert need > 0
+    ws = torch.full((need,), 255, dtype=torch.uint8, device=DEV)
+    want = [attend(c, q) for c, q in zip(caches, qs)]
+    graphs, outs = [], []
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for c, q in zip(caches, qs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            outs.append(attend(c, q, workspace=ws))
+        graphs.append(g)
+    torch.cuda.current_stream().wait_stream(side)
+    for i in (0, 1, 1, 0, 1, 0, 0):
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i][0], want[i][0]) and torch.equal(outs[i][1], want[i][1])
+        eager = attend(caches[1 - i], qs[1 - i], workspace=ws)
+        assert torch.equal(eager[0], want[1 - i][0])
+        outs[i][0].zero_()
+
+
+def test_bookkeeping_with_the_callers_buffers(gpu_lib):
+    """Every output and the workspace given, on a stream of its own; the same buffers again for a smaller step."""
+    import paper_2607_03612_amd as P
+
+    side = torch.cuda.Stream()
+    for R, in_place in ((2000, False), (1500, True), (40, False)):
+        args = random_step(R, R, 16, 4, R, 9, R // 10)
+        want = O.page_tables(*args)
+        lengths, new, free, table, count = ints(args[0]), ints(args[1]), ints(args[2]), ints(args[4]), ints([args[3]])
+        outs = dict(lengths_out=lengths if in_place else ints(np.zeros(R)), token_start=ints(np.zeros(R + 1)),
+                    slots=ints(np.zeros(args[6])), free_count_out=ints([0]))
+        need = P.page_tables_workspace_bytes(R, 16, 4, len(args[2]), args[6], in_place)
+        assert (need > 0) == (R > 1024)
+        ws = torch.full((max(need, 1),), 255, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        got = P.page_tables(lengths, new, free, count, table, 16, args[6], workspace=ws, stream=side, **outs)
+        side.synchronize()
+        for x, y in zip(got, (outs["lengths_out"], outs["token_start"], outs["slots"], outs["free_count_out"])):
+            assert x is y
+        np.testing.assert_array_equal(outs["slots"].cpu().numpy(), want["slots"])
+        np.testing.assert_array_equal(outs["lengths_out"].cpu().numpy(), want["lengths"])
+        np.testing.assert_array_equal(table.cpu().numpy(), want["table"])
+        assert int(outs["free_count_out"]) == want["count"]
