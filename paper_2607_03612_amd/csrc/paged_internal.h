@@ -109,16 +109,17 @@ constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / 64;
 
 // Rows are not shared out where the longest that the table has room for (the
-// lengths themselves are the GPU's) is this short: us, whole rows / shared out, 8
-// rows of four query heads at 128, 256, 512 KB: bf16 of dimension 64 6.0 / 10.9,
-// 8.6 / 11.0, 13.7 / 10.9; of dimension 128 5.9 / 9.9, 8.3 / 11.0, 12.6 / 11.1; fp32
-// 6.8 / 10.9, 10.1 / 12.6, 16.2 / 12.7; 8 bits 7.1 / 11.9, 10.9 / 12.9, 16.8 / 13.1;
-// 1024 rows at 256 and 512 KB: 33 / 38, 59 / 62 (bf16, 64). Shared out costs a
-// second launch, about 6 us of the host's time.
-constexpr int64_t kWholeRowBytes = 384 << 10;
+// lengths themselves are the GPU's) is this short, a CU's intake being 40 to 60 bytes
+// a ns, less in 8 bits. us, whole rows / shared out, 8 rows of four query heads at 256,
+// 384, 512 KB: bf16 of dimension 64 8.2 / 10.2, 10.8 / 10.4, 13.4 / 10.3; of dimension
+// 128 7.9 / 10.8, 10.1 / 11.1, 12.2 / 10.9; fp32 8.9 / 11.7, 11.6 / 11.8, 14.5 / 11.8; 8
+// bits of dimension 128 10.3 / 10.8, 13.4 / 10.8, 16.6 / 10.8; 128 rows at 384 KB 11.3 /
+// 14.6 (bf16, 128), 1024 rows 48.6 / 49.2. Shared out takes a second launch, about 4 us
+// of the host's time.
+constexpr int64_t kWholeRowBytes = 384 << 10, kWholeRowBytes8 = 256 << 10;
 inline bool whole_rows(int dtype, int dim, const DecodeArgs& a) {
   const int size = dtype == 0 ? 4 : dtype == 1 ? 2 : 1;
-  return (int64_t)a.max_pages * a.page.size * dim * size * 2 <= kWholeRowBytes &&
+  return (int64_t)a.max_pages * a.page.size * dim * size * 2 <= (dtype == 2 ? kWholeRowBytes8 : kWholeRowBytes) &&
          (int64_t)a.requests * a.kv_heads * a.qtiles <= kMaxWholeRows;
 }
 

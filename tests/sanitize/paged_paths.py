@@ -52,7 +52,7 @@ def test_page_tables(requests, tokens, in_place, launches):
 
 @pytest.mark.parametrize("dtype,size,dim,page,width,launches", [
     (0, 4, 64, 64, 12, 1), (0, 4, 64, 64, 13, 2), (1, 2, 128, 16, 48, 1), (1, 2, 128, 16, 49, 2), (2, 1, 128, 1024, 1, 1),
-    (2, 1, 128, 1024, 2, 2), (1, 2, 64, 1024, 1 << 19, 2)])
+    (2, 1, 128, 1024, 2, 2), (2, 1, 64, 128, 16, 1), (2, 1, 64, 128, 17, 2), (1, 2, 64, 1024, 1 << 19, 2)])
 @pytest.mark.parametrize("heads", [(1, 1), (256, 1), (256, 256), (96, 2)])
 def test_attention(dtype, size, dim, page, width, launches, heads):
     hq, hk = heads
