@@ -105,13 +105,14 @@ def _check_device(device):
         raise ValueError("expected device tensors")
 
 
-def _allocated(stream, *tensors):
-    """Memory of the current stream that the call allocated, for use on `stream`:
-    not before the current stream is done with what lay there, and not handed out
-    again before `stream` is."""
-    if stream is not None and any(t is not None for t in tensors):
-        binding._after_current(stream)
-        binding._keep_until_done(stream, *(t for t in tensors if t is not None))
+def _allocated(stream, device, tensors):
+    """Memory that the call allocated on the device's current stream, for use on
+    `stream`: not before the current one is done with what lay there, and not
+    handed out again before `stream` is."""
+    current = torch.cuda.current_stream(device)
+    if tensors and stream.cuda_stream != current.cuda_stream:
+        binding._torch_stream(stream).wait_stream(current)
+        binding._keep_until_done(stream, *tensors)
 
 
 def _given_workspace(t, device):
@@ -173,15 +174,15 @@ def page_tables(lengths, new_tokens, free_pages, free_count, page_table, page_si
     else:
         nbytes = _given_workspace(workspace, dev)
     if stream is not None:
-        _allocated(stream, *made)
+        _allocated(stream, dev, made)
     _call(lib.saf3r_page_tables, dev, stream, ctypes.byref(step), lengths_at, new_tokens.data_ptr(), free_pages.data_ptr(),
           count_at, page_table.data_ptr(), lengths_to, count_to, outs[1].data_ptr(), outs[2].data_ptr(), _ptr(workspace), nbytes)
     return tuple(outs)
 
 
 def _same_strides(s, t):
-    """Whether two tensors of one shape have the same strides; along one entry they say nothing."""
-    return s.stride() == t.stride() or all(x == y or n == 1 for x, y, n in zip(s.stride(), t.stride(), s.shape))
+    """Whether two tensors of one shape have the same strides but along single entries, where they say nothing."""
+    return all(x == y or n == 1 for x, y, n in zip(s.stride(), t.stride(), s.shape))
 
 
 def _layout(k_pages, v_pages, k_exp, v_exp):
@@ -193,7 +194,8 @@ def _layout(k_pages, v_pages, k_exp, v_exp):
     _check_device(dev)
     if len(shape) != 4 or strides[3] != 1:
         raise ValueError("pages must be [pages, kv_heads, page_size, head_dim], head_dim contiguous")
-    if v_pages.shape != shape or v_pages.dtype != dtype or v_pages.device != dev or not _same_strides(k_pages, v_pages):
+    if v_pages.shape != shape or v_pages.dtype != dtype or v_pages.device != dev \
+            or (v_pages.stride() != strides and not _same_strides(k_pages, v_pages)):
         raise ValueError("k_pages and v_pages must share shape, strides, dtype and device")
     n, H, ps, D = shape
     if code == E4M3:
@@ -227,7 +229,7 @@ def cache_append(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=N
     dev, shape, strides = k.device, k.shape, k.stride()
     if k.dtype != kind or dev != k_pages.device or len(shape) != 3 or strides[2] != 1:
         raise ValueError(f"k and v must be {kind} tensors [kv_heads, tokens, head_dim] on {k_pages.device}, head_dim contiguous")
-    if v.shape != shape or v.dtype != kind or v.device != dev or not _same_strides(k, v):
+    if v.shape != shape or v.dtype != kind or v.device != dev or (v.stride() != strides and not _same_strides(k, v)):
         raise ValueError("k and v must share shape, strides, dtype and device")
     H, T, D = shape
     if H != layout.kv_heads or D != layout.head_dim:
@@ -288,7 +290,10 @@ def paged_attention(q, k_pages, v_pages, page_table, lengths, k_exp=None, v_exp=
     if to[2] != 1:
         raise ValueError("out's head_dim must be contiguous")
     _check_apart("the rows of out", out)
-    lse = torch.empty((Hq, R), dtype=torch.float32, device=dev) if want_lse else None
+    lse = None
+    if want_lse:
+        lse = torch.empty(Hq, R, dtype=torch.float32, device=dev)
+        made.append(lse)
     step = Decode(R, Hq, width, anchor, window, D ** -0.5 if scale is None else scale, strides[0], strides[1], to[0], to[1])
     if workspace is None:
         nbytes = _attention_workspace(layout.dtype, layout.kv_heads, layout.page_size, D, Hq, R, width)
@@ -299,7 +304,7 @@ def paged_attention(q, k_pages, v_pages, page_table, lengths, k_exp=None, v_exp=
     else:
         nbytes = _given_workspace(workspace, dev)
     if stream is not None:
-        _allocated(stream, lse, *made)
+        _allocated(stream, dev, made)
     _call(lib.saf3r_paged_attention, dev, stream, ctypes.byref(layout), ctypes.byref(step), q.data_ptr(), k_pages.data_ptr(),
           v_pages.data_ptr(), _ptr(k_exp), _ptr(v_exp), page_table.data_ptr(), lengths.data_ptr(), out.data_ptr(), _ptr(lse),
           _ptr(workspace), nbytes)
