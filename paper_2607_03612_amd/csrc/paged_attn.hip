@@ -603,12 +603,13 @@ __device__ inline int run_of(int64_t total, int64_t x) {
   return total < (int64_t)kWaves * kMinTiles ? (int)(x / kMinTiles) : (int)(((x + 1) * kWaves - 1) / total);
 }
 
-// The outputs of requests without a token, every kWorkgroups-th request.
+// The outputs of requests without a token, every kWorkgroups-th request; `first` is
+// the first one's length.
 template <int kType, int kDim>
 __device__ inline void zero_rows(const DecodeArgs& a, const int32_t* __restrict__ lengths, char* __restrict__ out,
-                                 float* __restrict__ lse, int w) {
+                                 float* __restrict__ lse, int w, int32_t first) {
   for (int r = w; r < a.requests; r += kWorkgroups) {
-    if (lengths[r] > 0) continue;
+    if ((r == w ? first : lengths[r]) > 0) continue;
     for (int i = threadIdx.x; i < a.q_heads * (kDim / 4); i += kThreads) {
       const float none[4] = {0, 0, 0, 0};
       put_output<kType, 4>(a, out, lse, r, i / (kDim / 4), i % (kDim / 4) * 4, none, -INFINITY, 0.0f);
@@ -619,12 +620,16 @@ __device__ inline void zero_rows(const DecodeArgs& a, const int32_t* __restrict_
 struct PartHead {
   int32_t r;
   int32_t first, heads;
-  int32_t ends;    // 1: the row's last tile is in it; 0: not; -1: no part
-  int32_t behind;  // tiles of the row behind it
+  int32_t behind;  // tiles of the row behind the part
 };
 
 // The tiles of all requests' rows, request by request and row by row, are dealt out
-// to the waves in equal runs of neighbouring tiles.
+// to the waves in equal runs of neighbouring tiles. Bound by HBM where the runs are
+// long: one sequence of 274800 tokens 191 us with 16 heads of 64 in bf16 (5.9 TB/s of K
+// and V), 64 of up to 10992 with 8 heads of 128 249 us (5.8), 192 in 8 bits 382 (5.7).
+// Of a short launch 2 us go into counting and seeking, 1 to 4 into the first page and
+// its K, 1 into the parts; the waves of a full chip end within 6 us of one another,
+// those that came to the memory first ahead.
 template <int kType, int kDim>
 __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
     const char* __restrict__ q, const char* __restrict__ k, const char* __restrict__ v,
@@ -642,11 +647,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
     Parts<kDim, kSlots> parts;
   } lds;
   __shared__ PartHead heads_of[kSlots];
+  __shared__ int32_t ends_of[kSlots];  // 1: the row's last tile is in the part; 0: not; -1: no part
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rows = a.kv_heads * a.qtiles;
   const int w = blockIdx.x;
   const Pieces pc = pieces(workspace, piece_heads(a));
 
+  const int32_t own_length = w < a.requests ? lengths[w] : 1;
   // where the runs lie: each thread counts neighbouring requests
   const int each = (a.requests + kThreads - 1) / kThreads;
   int64_t mine = 0;
@@ -664,7 +671,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
     if (lane >= d) sum += y;
   }
   if (lane == 63) lds.deal.wave_sum[wave] = sum;
-  if (threadIdx.x < kSlots) heads_of[threadIdx.x].ends = -1;
+  if (threadIdx.x < kSlots) ends_of[threadIdx.x] = -1;
   __syncthreads();
   int64_t total = 0;
 #pragma unroll
@@ -677,7 +684,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
 
   if (threadIdx.x == 0) pc.cut[w].z = -1;
   if (run_start<S::kMinTiles>(total, w * kGroupWaves) >= total) {  // the whole workgroup
-    zero_rows<kType, kDim>(a, lengths, out, lse, w);
+    zero_rows<kType, kDim>(a, lengths, out, lse, w, own_length);
     return;
   }
   const int64_t lo = run_start<S::kMinTiles>(total, w * kGroupWaves + wave);
@@ -696,9 +703,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
       off -= (int64_t)next.s.count * rows;
       next.s = span_of<S::kTile>(a, lengths[++next.r]);
     }
-    const int32_t row = __builtin_amdgcn_readfirstlane((int32_t)(off / next.s.count));
+    // a division of 64 bits is a tenth of the time before the first load
+    const int32_t row = __builtin_amdgcn_readfirstlane(
+        off >> 32 == 0 ? (int32_t)((uint32_t)off / (uint32_t)next.s.count) : (int32_t)(off / next.s.count));
     next.x = __builtin_amdgcn_readfirstlane((int32_t)(off - (int64_t)row * next.s.count));
-    next.h = row / a.qtiles;
+    next.h = a.qtiles == 1 ? row : row / a.qtiles;
     next.qt = row - next.h * a.qtiles;
     next.set_row(a);
   }
@@ -720,7 +729,10 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
           } else {
             const int slot = 2 * wave + (from_start ? 1 : 0);
             put_part<kType>(lds.parts, slot, st);
-            if (lane == 0) heads_of[slot] = PartHead{p.r, p.first, p.heads, ends ? 1 : 0, p.s.count - 1 - p.x};
+            if (lane == 0) {
+              heads_of[slot] = PartHead{p.r, p.first, p.heads, p.s.count - 1 - p.x};
+              ends_of[slot] = ends ? 1 : 0;
+            }
           }
         });
   }
@@ -731,21 +743,26 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
   const int c = threadIdx.x >> 4, d = (threadIdx.x & 15) * kWidth;
   Sums<kWidth> sums;
   bool open = false, begun = false;
+  int32_t ends[kSlots];
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) ends[i] = __builtin_amdgcn_readfirstlane(ends_of[i]);
+  int last = -1;  // the last slot that holds a part
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) last = ends[i] >= 0 ? i : last;
+#pragma unroll
   for (int slot = 0; slot < kSlots; ++slot) {
-    const PartHead h = heads_of[slot];
-    if (h.ends < 0) continue;
+    if (ends[slot] < 0) continue;
     if (!open) {
       sums.clear();
       begun = (slot & 1) != 0;
       open = true;
     }
     sums.add(&lds.parts.o[slot][c][d], lds.parts.ml[slot][c]);
-    bool more = false;  // of the row in this workgroup
-    for (int s2 = slot + 1; s2 < kSlots && h.ends == 0; ++s2) more = more || heads_of[s2].ends >= 0;
-    if (more) continue;
+    if (ends[slot] == 0 && slot < last) continue;  // the row goes on in this workgroup
     open = false;
+    const PartHead h = heads_of[slot];
     const bool mine_too = c < h.heads;
-    if (begun && h.ends == 1) {
+    if (begun && ends[slot] == 1) {
       if (mine_too) put_output<kType, kWidth>(a, out, lse, h.r, h.first + c, d, sums.o, sums.m, sums.l);
     } else {
       if (mine_too) {
@@ -761,11 +778,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
       }
     }
   }
-  zero_rows<kType, kDim>(a, lengths, out, lse, w);
+  zero_rows<kType, kDim>(a, lengths, out, lse, w, own_length);
 }
 
 // The rows that fell to several workgroups, in the order of these: one workgroup per
-// such row and query; its 16-byte lanes take kThreads * 4 / kDim pieces at a time.
+// such row and query; its 16-byte lanes take kThreads * 4 / kDim pieces at a time. 2.7
+// to 4.9 us: the latency of the list, the pieces and the last sums.
 template <int kType, int kDim>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const void* __restrict__ workspace, char* __restrict__ out,
                                                               float* __restrict__ lse, DecodeArgs a) {
@@ -800,7 +818,9 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const void* __rest
 // --------------------------------------------------------------- whole rows
 
 // One workgroup per row: its waves take equal runs of the row's tiles and add up in
-// LDS. No counting, no pieces, no second launch.
+// LDS. No counting, no pieces, no second launch. Bound by one CU's intake where rows
+// are few (whole_rows), by HBM where they are many: 1024 rows of up to 261 tokens of 4
+// heads of 64 in bf16, 35 MB, 10 us.
 template <int kType, int kDim>
 __global__ __launch_bounds__(kRowThreads, 2) void paged_rows_kernel(
     const char* __restrict__ q, const char* __restrict__ k, const char* __restrict__ v,
