@@ -736,7 +736,7 @@ const char* saf3r_status_string(int32_t status) {
   switch (status) {
     case SAF3R_OK: return "ok";
     case SAF3R_ERR_INVALID_ARGUMENT: return "invalid argument (null or misaligned pointer, size or dtype)";
-    case SAF3R_ERR_UNSUPPORTED: return "unsupported (head_dim/block must be 64; size limits)";
+    case SAF3R_ERR_UNSUPPORTED: return "unsupported (head_dim, block or page size, or beyond the size limits)";
     case SAF3R_ERR_CAPACITY: return "index capacity or workspace smaller than required";
     case SAF3R_ERR_HIP: return "HIP runtime error on launch";
     case SAF3R_ERR_BAD_TABLE: return "bad pattern table (class or class parameter)";
