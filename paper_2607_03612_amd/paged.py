@@ -121,9 +121,14 @@ def _given_workspace(t, device):
     return t.numel() * t.element_size()
 
 
+@functools.lru_cache(maxsize=256)
+def _step_workspace(*sizes) -> int:
+    """The library's own answer, which these sizes alone decide."""
+    return _lib().saf3r_page_tables_workspace_bytes(ctypes.byref(PageStep(*sizes)))
+
+
 def page_tables_workspace_bytes(requests, page_size, max_pages, pages, tokens, in_place=False) -> int:
-    step = PageStep(requests, page_size, max_pages, pages, tokens, int(in_place))
-    r = _lib().saf3r_page_tables_workspace_bytes(ctypes.byref(step))
+    r = _step_workspace(requests, page_size, max_pages, pages, tokens, int(in_place))
     binding._check(min(r, 0), "saf3r_page_tables_workspace_bytes")
     return int(r)
 
@@ -153,20 +158,25 @@ def page_tables(lengths, new_tokens, free_pages, free_count, page_table, page_si
     _check_words("free_pages", free_pages, (pages,), dev)
     _check_words("free_count", free_count, (1,), dev)
     _check_words("page_table", page_table, (R, width), dev)
-    outs, made = [], []
-    for name, t, n in (("lengths_out", lengths_out, R), ("token_start", token_start, R + 1), ("slots", slots, tokens),
-                       ("free_count_out", free_count_out, 1)):
-        if t is None:
-            t = torch.empty(n, dtype=torch.int32, device=dev)
-            made.append(t)
-        else:
-            _check_words(name, t, (n,), dev)
-        outs.append(t)
+    outs, made = [lengths_out, token_start, slots, free_count_out], []
+    sizes = (R, R + 1, tokens, 1)
+    if lengths_out is None and token_start is None and slots is None and free_count_out is None:
+        # one allocation and its parts: a microsecond less than four
+        made.append(torch.empty(2 * R + tokens + 2, dtype=torch.int32, device=dev))
+        outs = made[0].split(sizes)
+    else:
+        for i, name in enumerate(("lengths_out", "token_start", "slots", "free_count_out")):
+            if outs[i] is None:
+                outs[i] = torch.empty(sizes[i], dtype=torch.int32, device=dev)
+                made.append(outs[i])
+            else:
+                _check_words(name, outs[i], (sizes[i],), dev)
     lengths_at, count_at = lengths.data_ptr(), free_count.data_ptr()
     lengths_to, count_to = outs[0].data_ptr(), outs[3].data_ptr()
-    step = PageStep(R, page_size, width, pages, tokens, 1 if lengths_at == lengths_to or count_at == count_to else 0)
+    in_place = 1 if lengths_at == lengths_to or count_at == count_to else 0
+    step = PageStep(R, page_size, width, pages, tokens, in_place)
     if workspace is None:
-        nbytes = lib.saf3r_page_tables_workspace_bytes(ctypes.byref(step))
+        nbytes = _step_workspace(R, page_size, width, pages, tokens, in_place)
         binding._check(min(nbytes, 0), "saf3r_page_tables")
         if nbytes > 0:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
