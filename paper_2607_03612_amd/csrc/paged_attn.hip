@@ -253,9 +253,7 @@ __device__ inline uint32_t fp8_pair(uint32_t codes, bool high, float scale) {
 }
 // Two fp32 as bf16 (nearest, ties to even), the first in the low half.
 __device__ inline uint32_t bf16_pair(float x, float y) {
-  uint32_t r;
-  asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
-  return r;
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
 }
 
 // S^T of a tile.
