@@ -17,18 +17,23 @@ constexpr int64_t kMaxStepTokens = (int64_t)1 << 30;
 constexpr int64_t kMaxAppendTokens = (int64_t)1 << 26;
 constexpr int64_t kMaxWholeRows = (int64_t)1 << 23;
 
-// x / page_size for 0 <= x < 2^29 + kMaxPageSize, as one high product: with d =
-// page_size / 16 <= 64 and m = ceil(2^31 / d), floor(x / 16) * (m d - 2^31) < 2^31.
+// x / page_size for 0 <= x < 2^31, as one high product and a shift: with d =
+// page_size / 16, l = floor(log2 d) and m = ceil(2^(31 + l) / d) < 2^32 (2^31 where d is
+// a power of two), m d is less than d above 2^(31 + l), and floor(x / 16) < 2^27 times
+// that is below 2^27 * 2^(l + 1) < 2^(31 + l): never a whole quotient too many.
 struct PageDiv {
-  uint32_t magic;  // ceil(2^31 / (page_size / 16)), at most 2^31
+  uint32_t magic;  // m
+  int32_t shift;   // l
   int32_t size;
 };
 inline PageDiv page_div(int32_t page_size) {
   const uint32_t d = (uint32_t)page_size / kPageQuantum;
-  return PageDiv{(uint32_t)((((uint64_t)1 << 31) + d - 1) / d), page_size};
+  int32_t l = 0;
+  while (d >> (l + 1)) ++l;
+  return PageDiv{(uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), l, page_size};
 }
 __host__ __device__ inline int32_t div_page(PageDiv p, int32_t x) {
-  return (int32_t)(((uint64_t)(((uint32_t)x >> 4) << 1) * p.magic) >> 32);
+  return (int32_t)((uint32_t)(((uint64_t)(((uint32_t)x >> 4) << 1) * p.magic) >> 32) >> p.shift);
 }
 
 // ---------------------------------------------------------------- page tables

@@ -31,6 +31,21 @@ def test_page_division_is_exact(size):
         assert div(size, x) == x // size, (size, x)
 
 
+@pytest.mark.parametrize("size", list(range(16, 1025, 16)))
+def test_page_division_is_exact_for_every_slot(size):
+    """Slots go up to 2^31 - 1. A reciprocal that is rounded up gives a page too many first at a page's last
+    place, and the later the page the sooner."""
+    div = lib().saf3r_stub_div_page
+    rng = random.Random(-size)
+    top = 2 ** 31 - 1
+    most = (top + 1) // size  # whole pages
+    firsts = [1, 2, most - 1, most] + [rng.randint(1, most) for _ in range(300)] + [most - i for i in range(300) if most > i]
+    xs = [top] + [m * size + d for m in firsts for d in (-1, 0)] + [rng.randint(0, top) for _ in range(300)]
+    for x in xs:
+        if x <= top:
+            assert div(size, x) == x // size, (size, x)
+
+
 @pytest.mark.parametrize("requests,tokens,in_place,launches", [
     (1, 0, 0, 1), (1024, 1 << 30, 0, 1), (1024, 4096, 1, 1), (1024, 4097, 1, 2), (1025, 1, 0, 2), (65536, 1 << 30, 1, 2)])
 def test_page_tables(requests, tokens, in_place, launches):

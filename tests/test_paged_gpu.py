@@ -691,3 +691,39 @@ def test_bookkeeping_with_the_callers_buffers(gpu_lib):
         np.testing.assert_array_equal(outs["lengths_out"].cpu().numpy(), want["lengths"])
         np.testing.assert_array_equal(table.cpu().numpy(), want["table"])
         assert int(outs["free_count_out"]) == want["count"]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("ps", [736, 992, 1008, 1024])
+def test_append_into_the_last_of_two_thousand_million_slots(gpu_lib, dtype, ps):
+    """Slots up to 2^31 - 1, a page's last and first ones. The pages share memory so that they fit: place o of page p
+    lies where p + o says, apart for the slots written here."""
+    import paper_2607_03612_amd as P
+
+    print(f"[last slots] {dtype} page {ps}", flush=True)
+    H, D = 2, 64
+    pages = (2 ** 31 - 1) // ps
+    rows = pages + ps  # of a head's memory
+    kv = [torch.zeros((H, rows, D), dtype=TYPES[dtype], device=DEV) for _ in range(2)]
+    views = [torch.as_strided(x, (pages, H, ps, D), (D, rows * D, D, 1)) for x in kv]
+    exps = [torch.full((pages, H, ps), 7, dtype=torch.uint8, device=DEV) for _ in range(2)] if dtype == "e4m3" else [None] * 2
+    border = np.arange(3 * ps, pages, 3 * ps)  # first slots of pages, and the ones before them
+    slots = np.concatenate([border * ps, border * ps - 1, [pages * ps - 1]])
+    page, at = slots // ps, slots % ps
+    assert len(set(page + at)) == len(slots)
+    wide = torch.float32 if dtype == "f32" else torch.bfloat16
+    g = torch.Generator(device=DEV).manual_seed(ps)
+    x = [torch.randn((H, len(slots), D), generator=g, device=DEV).to(wide) for _ in range(2)]
+    P.cache_append(x[0], x[1], ints(slots), views[0], views[1], *exps)
+    where = torch.from_numpy(page + at).to(DEV)
+    for tokens, got, e in zip(x, kv, exps):
+        want = torch.zeros_like(got)
+        if dtype == "e4m3":
+            codes, exp = O.quantise(tokens.double().cpu().numpy())
+            want.view(torch.uint8)[:, where] = torch.from_numpy(codes).to(DEV)
+            full = torch.full_like(e, 7)
+            full[torch.from_numpy(page).to(DEV), :, torch.from_numpy(at).to(DEV)] = torch.from_numpy(exp.T.copy()).to(DEV)
+            assert torch.equal(e, full)
+        else:
+            want[:, where] = tokens
+        assert torch.equal(got.view(torch.uint8), want.view(torch.uint8))
