@@ -175,7 +175,8 @@ saf3r_status saf3r_cache_append(const saf3r_page_layout* cache, const saf3r_toke
  *   workspace       saf3r_paged_attention_workspace_bytes, 16-byte aligned; may be
  *                   NULL if these are 0
  * Limits: q_heads 1 .. 256 and a multiple of kv_heads, requests 1 .. 65536,
- * max_pages * page_size <= 2^29, anchor >= 0, window >= 0, scale finite and > 0. */
+ * max_pages * page_size <= 2^29, anchor >= 0, window >= 0, scale > 0 and
+ * scale * log2(e) finite in fp32. */
 typedef struct {
   int32_t requests;
   int32_t q_heads;

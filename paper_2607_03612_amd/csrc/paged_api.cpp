@@ -65,7 +65,8 @@ saf3r_status check_decode(const saf3r_page_layout* cache, const saf3r_decode* d,
   if (st != SAF3R_OK) return st;
   if (!d || d->requests <= 0 || d->q_heads <= 0 || d->max_pages <= 0 || d->anchor < 0 || d->window < 0)
     return SAF3R_ERR_INVALID_ARGUMENT;
-  if (!(d->scale > 0.0f) || !isfinite(d->scale)) return SAF3R_ERR_INVALID_ARGUMENT;
+  const float scale_log2 = d->scale * 1.4426950408889634f;  // log2(e)
+  if (!(d->scale > 0.0f) || !isfinite(scale_log2)) return SAF3R_ERR_INVALID_ARGUMENT;
   if (d->requests > saf3r::kMaxRequests || d->q_heads > saf3r::kMaxPagedHeads || d->q_heads % cache->kv_heads != 0 ||
       (int64_t)d->max_pages * cache->page_size > saf3r::kMaxRowTokens)
     return SAF3R_ERR_UNSUPPORTED;
@@ -86,7 +87,7 @@ saf3r_status check_decode(const saf3r_page_layout* cache, const saf3r_decode* d,
   a->pages = cache->pages;
   a->anchor = d->anchor;
   a->window = d->window;
-  a->scale_log2 = d->scale * 1.4426950408889634f;
+  a->scale_log2 = scale_log2;
   a->page = saf3r::page_div(cache->page_size);
   a->token_stride = (int32_t)c->token;
   a->page_stride = c->page;

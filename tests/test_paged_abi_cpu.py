@@ -140,3 +140,11 @@ def test_append_refuses(G):
     assert run(ke=OK) == -1 and run(layout(G, dtype=2), ke=OK) == -1 and run(layout(G, dtype=2), ke=A2, ve=OK) == -1
     # nothing to write needs no tokens
     assert run(rows=(0, 0, 64, 64), k=None, v=None, slots=None) == 0
+
+
+def test_scales_whose_product_with_log2_e_is_not_finite(G):
+    """The kernels work in powers of two: an infinite factor would make the score 0 * inf of a zero query NaN."""
+    size = lib_of(G).saf3r_paged_attention_workspace_bytes
+    for scale, want in ((3e38, -1), (2.4e38, -1), (2.3e38, 1), (1e-45, 1)):
+        got = size(ctypes.byref(layout(G)), ctypes.byref(decode(G, scale=scale)))
+        assert got == want if want < 0 else got > 0, scale
