@@ -23,7 +23,8 @@
  * workspaces do not overlap. A workspace is overwritten and holds nothing
  * between calls; calls that share one must be ordered on the GPU.
  *
- * Strides count elements; a stride along a dimension of one entry is not looked at.
+ * Strides count elements; a stride along a dimension of one entry is not looked at. Along
+ * n entries it is at most 2^44 bytes, and n times it at most 2^60.
  *
  * What the GPU reads from lengths, tables and slots is bounded there: a bad
  * entry gives no access outside the arrays, as each call says.

@@ -25,7 +25,12 @@ int64_t stride_bytes(int64_t stride, int64_t n, int size, int64_t limit) {
   if (stride < 0 || stride > limit / size || stride * size % 16 != 0) return -1;
   return stride * size;
 }
-constexpr int64_t kMaxStride = (int64_t)1 << 44;  // bytes, past any device's memory: products of strides and indexes fit 63 bits
+// Past what entries in one device's memory can be apart, and under 2^60 bytes to the
+// last of them: sums of such products fit 63 bits.
+int64_t far_limit(int64_t n) {
+  const int64_t most = (int64_t)1 << 44, last = ((int64_t)1 << 60) / (n > 1 ? n : 1);
+  return most < last ? most : last;
+}
 
 struct Cache {
   int size;  // bytes of a value
@@ -41,8 +46,8 @@ saf3r_status check_cache(const saf3r_page_layout* c, Cache* out) {
   if (c->kv_heads > saf3r::kMaxPagedHeads) return SAF3R_ERR_UNSUPPORTED;
   if ((int64_t)c->pages * c->page_size > INT32_MAX) return SAF3R_ERR_UNSUPPORTED;
   out->size = c->dtype == SAF3R_CACHE_F32 ? 4 : c->dtype == SAF3R_CACHE_BF16 ? 2 : 1;
-  out->page = stride_bytes(c->page_stride, c->pages, out->size, kMaxStride >> 13);  // times up to 2^27 pages
-  out->head = stride_bytes(c->head_stride, c->kv_heads, out->size, kMaxStride);
+  out->page = stride_bytes(c->page_stride, c->pages, out->size, far_limit(c->pages));
+  out->head = stride_bytes(c->head_stride, c->kv_heads, out->size, far_limit(c->kv_heads));
   out->token = stride_bytes(c->token_stride, c->page_size, out->size, (((int64_t)1 << 30) - 1) / c->page_size);
   if (out->page < 0 || out->head < 0 || out->token < 0) return SAF3R_ERR_INVALID_ARGUMENT;
   return SAF3R_OK;
@@ -74,7 +79,8 @@ saf3r_status check_decode(const saf3r_page_layout* cache, const saf3r_decode* d,
   const int64_t strides[4] = {d->q_head_stride, d->q_request_stride, d->out_head_stride, d->out_request_stride};
   int64_t* to[4] = {&a->q_head, &a->q_request, &a->out_head, &a->out_request};
   for (int i = 0; i < 4; ++i) {
-    const int64_t bytes = stride_bytes(strides[i], i % 2 == 0 ? d->q_heads : d->requests, wide, kMaxStride);
+    const int64_t n = i % 2 == 0 ? d->q_heads : d->requests;
+    const int64_t bytes = stride_bytes(strides[i], n, wide, far_limit(n));
     if (bytes < 0) return SAF3R_ERR_INVALID_ARGUMENT;
     *to[i] = bytes / wide;
   }
@@ -152,8 +158,8 @@ saf3r_status saf3r_cache_append(const saf3r_page_layout* cache, const saf3r_toke
   if (rows->tokens > saf3r::kMaxAppendTokens) return SAF3R_ERR_UNSUPPORTED;
   const int wide = cache->dtype == SAF3R_CACHE_F32 ? 4 : 2;
   saf3r::AppendArgs a{};
-  a.row_head = stride_bytes(rows->head_stride, cache->kv_heads, wide, kMaxStride);
-  a.row_token = stride_bytes(rows->token_stride, rows->tokens, wide, kMaxStride >> 12);
+  a.row_head = stride_bytes(rows->head_stride, cache->kv_heads, wide, far_limit(cache->kv_heads));
+  a.row_token = stride_bytes(rows->token_stride, rows->tokens, wide, far_limit(rows->tokens));
   if (a.row_head < 0 || a.row_token < 0) return SAF3R_ERR_INVALID_ARGUMENT;
   if (!k_pages || !v_pages || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !exps_ok(cache->dtype, k_exp, v_exp))
     return SAF3R_ERR_INVALID_ARGUMENT;

@@ -91,3 +91,17 @@ def test_attention(dtype, size, dim, page, width, launches, heads):
         assert lib().saf3r_stub_paged_launches() == 2
     rows = G.TokenLayout(1 << 26, 0, dim, 0)
     assert lib().saf3r_cache_append(ctypes.byref(layout), ctypes.byref(rows), OK, OK, OK, OK, OK, *exps, None) == 0
+
+
+def test_far_apart_is_no_reason_to_refuse():
+    """Any stride that two entries in a device's memory can have; what would pass 63 bits is none."""
+    def run(pages, page_stride, tokens, token_stride):
+        layout = G.PageLayout(pages, 16, 2, 64, binding.BF16, 0, page_stride // 2, 1024, 64)
+        rows = G.TokenLayout(tokens, 0, 64, token_stride // 2)
+        return lib().saf3r_cache_append(ctypes.byref(layout), ctypes.byref(rows), OK, OK, OK, OK, OK, None, None, None)
+
+    for pages, tokens in ((2, 2), (1 << 24, 1 << 24)):
+        assert run(pages, 1 << 36, tokens, 4096) == 0 and run(pages, 4096, tokens, 1 << 36) == 0, pages
+    assert run(2, 1 << 44, 2, 1 << 44) == 0 and run(2, (1 << 44) + 16, 2, 16) == -1 and run(2, 16, 2, (1 << 44) + 16) == -1
+    assert run(1 << 26, 1 << 34, 1 << 26, 1 << 34) == 0
+    assert run(1 << 26, (1 << 34) + 16, 2, 16) == -1 and run(2, 16, 1 << 26, (1 << 34) + 16) == -1

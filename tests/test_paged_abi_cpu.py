@@ -148,3 +148,13 @@ def test_scales_whose_product_with_log2_e_is_not_finite(G):
     for scale, want in ((3e38, -1), (2.4e38, -1), (2.3e38, 1), (1e-45, 1)):
         got = size(ctypes.byref(layout(G)), ctypes.byref(decode(G, scale=scale)))
         assert got == want if want < 0 else got > 0, scale
+
+
+def test_far_apart_is_no_reason_to_refuse(G):
+    """Any stride that two entries in a device's memory can have."""
+    lib = lib_of(G)
+    size = lib.saf3r_paged_attention_workspace_bytes
+    far = 1 << 36  # bytes
+    for n, dtype, item in ((2, 1, 2), (1000, 0, 4), (1 << 20, 2, 1)):
+        pages = layout(G, pages=n, dtype=dtype, page_stride=far // item)
+        assert size(ctypes.byref(pages), ctypes.byref(decode(G))) > 0, n

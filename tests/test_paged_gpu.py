@@ -727,3 +727,32 @@ def test_append_into_the_last_of_two_thousand_million_slots(gpu_lib, dtype, ps):
         else:
             want[:, where] = tokens
         assert torch.equal(got.view(torch.uint8), want.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_pages_far_apart(gpu_lib, dtype):
+    """Pages and tokens more than 2^32 bytes apart."""
+    import paper_2607_03612_amd as P
+
+    size = 2 if dtype == "bf16" else 1
+    c = Cache(23, dtype, [40], 2, 64, 16, spare=0)
+    q = queries(17, 4, 1, 64, dtype)
+    want, want_lse = attend(c, q)
+    far = (1 << 32) // size + 4096
+    odd = []
+    for x in c.kv:
+        big = torch.zeros(2 * far + 2048, dtype=TYPES[dtype], device=DEV)
+        y = torch.as_strided(big, x.shape, (far, 1024, 64, 1))
+        word = torch.uint8 if size == 1 else torch.int16
+        y.view(word).copy_(x.view(word))
+        odd.append(y)
+    out, lse = P.paged_attention(q, odd[0], odd[1], c.table, c.lengths, *c.exps, want_lse=True)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    rows = torch.zeros((1 << 31) + 8192, dtype=torch.bfloat16, device=DEV)
+    k = torch.as_strided(rows, (2, 2, 64), (64, (1 << 31) + 4096, 1))
+    k.copy_(torch.randn((2, 2, 64), device=DEV))
+    slots = ints([2 * 16 + 9, 3])
+    P.cache_append(k, k, slots, odd[0], odd[1], *c.exps)
+    P.cache_append(k.contiguous(), k.contiguous(), slots, c.kv[0], c.kv[1], *c.exps)
+    for x, y in zip(odd, c.kv):
+        assert torch.equal(x.contiguous().view(torch.uint8), y.view(torch.uint8))
