@@ -95,6 +95,13 @@ def _check_int(name, x, low):
         raise ValueError(f"{name} must be in [{low}, 2^31)")
 
 
+def _check_sizes(*shapes):
+    """The library takes sizes as int32, and ctypes drops what does not fit."""
+    for shape in shapes:
+        if max(shape, default=0) > _INT_MAX:
+            raise ValueError("sizes must be below 2^31")
+
+
 def _check_words(name, t, shape, device):
     if t.dtype != torch.int32 or t.device != device or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor of shape {list(shape)} on {device}")
@@ -128,6 +135,7 @@ def _step_workspace(*sizes) -> int:
 
 
 def page_tables_workspace_bytes(requests, page_size, max_pages, pages, tokens, in_place=False) -> int:
+    _check_sizes([abs(x) for x in (requests, page_size, max_pages, pages, tokens)])
     r = _step_workspace(requests, page_size, max_pages, pages, tokens, int(in_place))
     binding._check(min(r, 0), "saf3r_page_tables_workspace_bytes")
     return int(r)
@@ -148,6 +156,7 @@ def page_tables(lengths, new_tokens, free_pages, free_count, page_table, page_si
     lib = _lib()
     _check_int("page_size", page_size, 1)
     _check_int("tokens", tokens, 0)
+    _check_sizes(lengths.shape, free_pages.shape, page_table.shape)
     dev = lengths.device
     _check_device(dev)
     if lengths.dim() != 1 or free_pages.dim() != 1 or page_table.dim() != 2:
@@ -235,6 +244,7 @@ def cache_append(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=N
     one, the latter with the exponents ``k_exp`` and ``v_exp``. Slots outside the
     cache (-1) are skipped; the others must be distinct."""
     lib = _lib()
+    _check_sizes(k.shape, k_pages.shape)
     layout, kind = _layout(k_pages, v_pages, k_exp, v_exp)
     dev, shape, strides = k.device, k.shape, k.stride()
     if k.dtype != kind or dev != k_pages.device or len(shape) != 3 or strides[2] != 1:
@@ -261,6 +271,7 @@ def _attention_workspace(code, kv_heads, page_size, head_dim, q_heads, requests,
 
 def paged_attention_workspace_bytes(q, k_pages, v_pages, page_table, k_exp=None, v_exp=None) -> int:
     _lib()
+    _check_sizes(q.shape, k_pages.shape, page_table.shape)
     c, _ = _layout(k_pages, v_pages, k_exp, v_exp)
     r = _attention_workspace(c.dtype, c.kv_heads, c.page_size, c.head_dim, q.shape[0], q.shape[1], page_table.shape[1])
     binding._check(min(r, 0), "saf3r_paged_attention_workspace_bytes")
@@ -280,6 +291,7 @@ def paged_attention(q, k_pages, v_pages, page_table, lengths, k_exp=None, v_exp=
     lib = _lib()
     _check_int("anchor", anchor, 0)
     _check_int("window", window, 0)
+    _check_sizes(q.shape, k_pages.shape, page_table.shape)
     layout, kind = _layout(k_pages, v_pages, k_exp, v_exp)
     dev, shape, strides = k_pages.device, q.shape, q.stride()
     if q.dtype != kind or q.device != dev or len(shape) != 3 or strides[2] != 1 or shape[2] != layout.head_dim:

@@ -64,6 +64,34 @@ def test_binding_refuses_numbers_out_of_range(G):
             G.page_tables(i(2), i(2), i(9), i(1), i(2, 4), size, tokens)
 
 
+def test_binding_refuses_sizes_past_32_bits(G):
+    """What the library takes as int32 must not arrive there without its upper half."""
+    big = 2 ** 32 + 1
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    for k in range(5):
+        sizes = [4, 16, 8, 100, 64]
+        for x in (big, sizes[k] - 2 ** 32):
+            sizes[k] = x
+            with pytest.raises(ValueError, match="2\\^31"):
+                G.page_tables_workspace_bytes(*sizes)
+    pages = torch.zeros((3, 2, 16, 64), dtype=torch.bfloat16)
+    many = pages[:1].expand(big, 2, 16, 64)
+    q = torch.zeros((2, 1, 64), dtype=torch.bfloat16)
+    for call in (lambda: G.paged_attention(q, many, many, i(1, 2), i(1)),
+                 lambda: G.paged_attention_workspace_bytes(q, many, many, i(1, 2)),
+                 lambda: G.cache_append(pages[0], pages[0], i(16), many, many),
+                 lambda: G.paged_attention_workspace_bytes(q.expand(2, big, 64), pages, pages, i(1, 2)),
+                 lambda: G.paged_attention_workspace_bytes(q[:1].expand(big, 1, 64), pages, pages, i(1, 2)),
+                 lambda: G.paged_attention(q.expand(2, big, 64), pages, pages, i(1, 2), i(1)),
+                 lambda: G.paged_attention(q, pages, pages, i(1, 1).expand(1, big), i(1)),
+                 lambda: G.cache_append(pages[0, :, :1].expand(2, big, 64), pages[0, :, :1].expand(2, big, 64), i(16), pages, pages),
+                 lambda: G.page_tables(i(1).expand(big), i(2), i(9), i(1), i(2, 4), 16, 3),
+                 lambda: G.page_tables(i(2), i(2), i(1).expand(big), i(1), i(2, 4), 16, 3),
+                 lambda: G.page_tables(i(2), i(2), i(9), i(1), i(2, 1).expand(2, big), 16, 3)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
+
+
 def test_binding_refuses_a_library_without_the_calls(G, monkeypatch):
     from paper_2607_03612_amd import binding
 
