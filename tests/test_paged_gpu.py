@@ -756,3 +756,28 @@ def test_pages_far_apart(gpu_lib, dtype):
     P.cache_append(k.contiguous(), k.contiguous(), slots, c.kv[0], c.kv[1], *c.exps)
     for x, y in zip(odd, c.kv):
         assert torch.equal(x.contiguous().view(torch.uint8), y.view(torch.uint8))
+
+
+def test_append_e4m3_past_four_gigabytes(gpu_lib):
+    """The codes and exponents of pages whose bytes lie past 2^32, and nothing else."""
+    import paper_2607_03612_amd as P
+
+    H, ps, D = 8, 64, 128
+    pages = (5 << 30) // (H * ps * D)
+    kv = [torch.zeros((pages, H, ps, D), dtype=torch.float8_e4m3fn, device=DEV) for _ in range(2)]
+    exps = [torch.full((pages, H, ps), 9, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    near = (1 << 32) // (H * ps * D)  # the page at 2^32
+    slots = np.array([pages * ps - 1, 5, (pages - 1) * ps, near * ps, near * ps - 1, (pages - 7) * ps + 33])
+    g = torch.Generator(device=DEV).manual_seed(8)
+    x = [(torch.randn((H, len(slots), D), generator=g, device=DEV) * 2.0 ** torch.arange(-9, -9 + 3 * len(slots), 3, device=DEV)[None, :, None])
+         .bfloat16() for _ in range(2)]
+    P.cache_append(x[0], x[1], ints(slots), kv[0], kv[1], exps[0], exps[1])
+    page, at = (torch.from_numpy(y).to(DEV) for y in (slots // ps, slots % ps))
+    for tokens, got, e in zip(x, kv, exps):
+        codes, exp = O.quantise(tokens.double().cpu().numpy())
+        bits = got.view(torch.uint8)
+        np.testing.assert_array_equal(bits[page, :, at].cpu().numpy(), codes.transpose(1, 0, 2))
+        np.testing.assert_array_equal(e[page, :, at].cpu().numpy(), exp.T)
+        bits[page, :, at] = 0
+        e[page, :, at] = 9
+        assert not bool(bits.view(torch.int64).any()) and bool((e == 9).all())
