@@ -4,6 +4,11 @@ The functions take torch tensors on the GPU and run on the tensors' device, on
 its current stream unless ``stream`` names another. As in ``binding``, every
 computation runs in the HIP library; the outputs and workspaces that a caller
 does not pass are allocated here.
+
+With ``stream``, what the caller passes is the caller's to order: inputs still
+being written on another stream, and tensors let go while ``stream`` reads them.
+Memory that the call allocates is ordered here, which makes ``stream`` wait for
+the device's current one; a call that allocates nothing does not wait.
 """
 from __future__ import annotations
 

@@ -781,3 +781,81 @@ def test_append_e4m3_past_four_gigabytes(gpu_lib):
         bits[page, :, at] = 0
         e[page, :, at] = 9
         assert not bool(bits.view(torch.int64).any()) and bool((e == 9).all())
+
+
+def shared_out_case():
+    """A call whose workspace, 4.3 MB, is the only block of its size."""
+    c = Cache(24, "bf16", [3000, 900], 2, 64, 16)
+    q = queries(18, 32, 2, 64, "bf16")
+    import paper_2607_03612_amd as P
+
+    need = P.paged_attention_workspace_bytes(q, c.kv[0], c.kv[1], c.table)
+    assert need > 1 << 22
+    return c, q, need
+
+
+def keep_busy(n=40):
+    """About 5 ms of the current stream; the matrices stay until the end."""
+    a = torch.randn((4096, 4096), device=DEV)
+    b = torch.empty_like(a)
+    for _ in range(n):
+        torch.mm(a, a, out=b)
+    return a, b
+
+
+def test_memory_of_a_call_on_another_stream_is_kept_until_it_is_done(gpu_lib):
+    """The workspace that such a call allocates and lets go is not handed out again while its stream is still busy; after a
+    call on the current stream it is."""
+    c, q, need = shared_out_case()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        keep_busy(1)
+    want, _ = attend(c, q)
+    torch.cuda.synchronize()
+
+    def block():
+        return torch.empty(need, dtype=torch.uint8, device=DEV)
+
+    at = block().data_ptr()  # the free block that the next call takes
+    out, _ = attend(c, q)
+    again = block()
+    assert again.data_ptr() == at
+    del again, out
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        busy = keep_busy()
+    out, _ = attend(c, q, stream=side)
+    done = torch.cuda.Event()
+    done.record(side)
+    again = block()
+    again.fill_(255)
+    assert not done.query(), "the other stream has to be busy here"
+    assert again.data_ptr() != at
+    side.synchronize()
+    assert torch.equal(out, want)
+    del busy
+
+
+def test_a_call_on_another_stream_waits_for_the_memory_that_it_allocates(gpu_lib):
+    """The current stream may still be at work on what lay in the block before."""
+    import paper_2607_03612_amd as P
+
+    c, q, need = shared_out_case()
+    step = random_step(3, 40, 16, 6, 90, 30, 4)
+    lengths, new, free, count, table = ints(step[0]), ints(step[1]), ints(step[2]), ints([step[3]]), ints(step[4])
+    side = torch.cuda.Stream()
+    want, _ = attend(c, q)
+    keep_busy(1)
+    for call in (lambda: attend(c, q, stream=side),
+                 lambda: P.page_tables(lengths, new, free, count, table, step[5], step[6], stream=side)):
+        torch.cuda.synchronize()
+        busy = keep_busy()
+        before = torch.cuda.Event()
+        before.record()
+        got = call()
+        assert not before.query(), "the current stream has to be busy here"
+        side.synchronize()
+        assert before.query()
+        if got[0].dtype == torch.bfloat16:
+            assert torch.equal(got[0], want)
+        del busy
