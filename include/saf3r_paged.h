@@ -147,7 +147,8 @@ saf3r_status saf3r_cache_append(const saf3r_page_layout* cache, const saf3r_toke
                                 void* v_pages, uint8_t* k_exp, uint8_t* v_exp, void* stream);
 
 /* Attention of one query token per request over the request's cached tokens.
- * Query head h reads key-value head h / (q_heads / kv_heads). For request r with
+ * Query head h reads key-value head h / (q_heads / kv_heads); K and V are read once for
+ * each 16 query heads that share them. For request r with
  * n = lengths[r] (read as 0 .. max_pages * page_size):
  *   z_j = scale * q . k_j   over the tokens j < n, with window > 0 only those with
  *                           j < anchor or j >= n - window
@@ -165,7 +166,9 @@ saf3r_status saf3r_cache_append(const saf3r_page_layout* cache, const saf3r_toke
  * its own rounding to bf16.
  * The keys of all requests are shared out evenly among the chip's workgroups,
  * whatever the lengths; the parts of a sequence that fell to several are joined
- * in a fixed order (same inputs, same bits).
+ * in a fixed order (same inputs, same bits). Where max_pages * page_size tokens of a
+ * head's K and V are at most 384 KB (256 KB in 8 bits), a workgroup takes each row whole
+ * instead, in one launch: a table no wider than its sequences is faster for short ones.
  *   q, out          element (h, r, d) at h * head_stride + r * request_stride + d;
  *                   strides >= 0, multiples of 16 bytes; 16-byte aligned; the rows
  *                   of out distinct

@@ -1,7 +1,8 @@
 """SAF3R block-sparse global attention for AMD Instinct MI355X (gfx950).
 
 The compute path is the HIP library ``libsaf3r.so`` (C ABI in
-``include/saf3r.h``); ``binding`` marshals torch device tensors into it.
+``include/saf3r.h`` and, for the paged key-value cache, ``include/saf3r_paged.h``);
+``binding`` and ``paged`` marshal torch device tensors into it.
 """
 from . import binding  # noqa: F401
 from .binding import (  # noqa: F401

@@ -157,10 +157,9 @@ __device__ inline int32_t take_pages(RequestRecord& rec, int32_t fresh, uint32_t
 // share of the pages given back; the first one writes what belongs to the requests. No
 // workgroup waits for another: a page that an ended sequence gave back is read from
 // that sequence's row, not from the stack. Bound by the chain of lengths, sums, table
-// and stores: 2.7 us for 64 requests and as many tokens, 7.1 for 1000 with 21000 tokens
-// and 37 that end. (Two launches, one to count and one with a
-// thread per token: 10.2 us for 1000 requests at 1024 to 16384 tokens where this takes
-// 5.2, and 4 us more of the host's time.)
+// and stores: 2.7 us for 64 requests and as many tokens, 7.2 for 1000 with 21000 tokens
+// and 37 that end. (Two launches, one to count and one with a thread per token: 10.3 us
+// for a request more than the 1024 that take 5.2 here, and 4 us more of the host's time.)
 template <int kThreads>
 __global__ __launch_bounds__(kThreads) void page_step_kernel(
     const int32_t* lengths, const int32_t* __restrict__ new_tokens, int32_t* free_pages, const int32_t* free_count,
@@ -218,8 +217,13 @@ __device__ inline void push_pages(int r, const Request& q, uint32_t count, int32
   }
 }
 
-// A step of any number of requests, kScanThreads a turn, by one workgroup; the slots
-// follow in a launch of their own. About 10 us up to 1024 requests in place.
+// A step of any number of requests, kScanThreads a turn, by one workgroup that goes over
+// them twice; the slots follow in a launch of their own. Bound by the chain of reads and
+// sums, about 1.2 us for a turn of one pass. Both launches: 6.7 us for 100 requests with
+// 137400 tokens in place, 10.3 for 1025 requests with a token each, 16 for 4096, 43 for
+// 16384, 150 for 65536. Pages that are given back come on top, a wave's ended requests
+// one after another: 7 us for 11300 pages of 128 requests among 4096, 73 for 23100 of
+// 2048 among 65536.
 constexpr int kScanThreads = 1024;
 __global__ __launch_bounds__(kScanThreads) void page_scan_kernel(
     const int32_t* lengths, const int32_t* __restrict__ new_tokens, int32_t* free_pages,

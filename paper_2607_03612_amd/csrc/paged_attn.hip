@@ -30,12 +30,13 @@ struct Shape {
   static constexpr int kSize = kType == 0 ? 4 : kType == 1 ? 2 : 1;  // bytes of a cached value
   static constexpr int kVDims = kDim / 16;                           // dimensions of V per lane
   // 16-key groups of a tile: 32 to 64 registers of K and V in flight per lane (four for
-  // bf16 of 64 as well: 16.7 -> 21.7 us for 1024 rows of 512 tokens)
+  // bf16 of 64 as well: 26.7 -> 28.3 us for 1024 rows of 512 tokens, 10.2 -> 9.7 for 128
+  // rows of 1024)
   static constexpr int kGroups = kType == 0 ? (kDim == 64 ? 2 : 1) : kType == 1 ? 2 : 4;
   static constexpr int kTile = 16 * kGroups;            // keys
-  // A wave's share in a shared-out launch is at least 64 keys: with half as many as
-  // that, 12.8 -> 13.5 us for 16 rows of 2100 tokens in fp32; with twice, 11.7 -> 14.2
-  // in 8 bits.
+  // A wave's share in a shared-out launch is at least 64 keys. For 16 rows of 2100
+  // tokens: with half as many as that, 12.4 -> 12.8 us in fp32 of 64, 11.8 -> 12.2 in bf16
+  // of 128; with twice, 12.4 -> 16.0, 11.8 -> 14.3 and in 8 bits of 128 11.1 -> 13.6.
   static constexpr int kMinTiles = 64 / kTile;
   static constexpr int kKWords = kDim * kSize / 16;     // words of K per lane and group
   static constexpr int kVWords = kVDims * kSize / 4;    // words of V per lane and key
@@ -623,8 +624,8 @@ struct PartHead {
 
 // The tiles of all requests' rows, request by request and row by row, are dealt out
 // to the waves in equal runs of neighbouring tiles. Bound by HBM where the runs are
-// long: one sequence of 274800 tokens 191 us with 16 heads of 64 in bf16 (5.9 TB/s of K
-// and V), 64 of up to 10992 with 8 heads of 128 249 us (5.8), 192 in 8 bits 382 (5.7).
+// long: one sequence of 274800 tokens 188 us with 16 heads of 64 in bf16 (6.0 TB/s of K
+// and V), 64 of up to 10992 with 8 heads of 128 247 us (5.8), 192 in 8 bits 382 (5.7).
 // Of a short launch 2 us go into counting and seeking, 1 to 4 into the first page and
 // its K, 1 into the parts; the waves of a full chip end within 6 us of one another,
 // those that came to the memory first ahead.
@@ -816,9 +817,11 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const void* __rest
 // --------------------------------------------------------------- whole rows
 
 // One workgroup per row: its waves take equal runs of the row's tiles and add up in
-// LDS. No counting, no pieces, no second launch. Bound by one CU's intake where rows
-// are few (whole_rows), by HBM where they are many: 1024 rows of up to 261 tokens of 4
-// heads of 64 in bf16, 35 MB, 10 us.
+// LDS. No counting, no pieces, no second launch. Bound by one CU's intake where rows are
+// few and long (whole_rows), by memory where they are many. Short ones wait for a chain
+// of latencies (a length, the table, K and V, the sums): requests of up to 261 tokens of 4
+// heads of 64 in bf16 take 5.3 us, be it one or 32, 256 of them (35 MB) 9.8, 1024 33 (4.3
+// TB/s), 2048 62 (4.6 TB/s).
 template <int kType, int kDim>
 __global__ __launch_bounds__(kRowThreads, 2) void paged_rows_kernel(
     const char* __restrict__ q, const char* __restrict__ k, const char* __restrict__ v,

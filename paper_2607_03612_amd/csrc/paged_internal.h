@@ -102,25 +102,29 @@ struct DecodeArgs {
   int64_t q_head, q_request, out_head, out_request;
 };
 
-// Shared-out launches: 512 workgroups of four waves, two waves to a SIMD (with 1024
-// 5 to 20% slower where a wave has few tiles, the same elsewhere).
+// Shared-out launches: 512 workgroups of four waves, two waves to a SIMD (with 1024, 8
+// sequences of 2100 tokens over 8 heads 20.0 -> 25.3 us in fp32 of 64, 16.7 -> 19.9 in 8
+// bits of 128; of 8192 55 -> 59 and 34 -> 39; 32 of 8192 190 -> 193 and 105 -> 105).
 constexpr int kThreads = 256;
 constexpr int kGroupWaves = kThreads / 64;
 constexpr int kWorkgroups = 512;
 constexpr int kWaves = kWorkgroups * kGroupWaves;  // a power of two
-// Whole-row launches: four waves share a row (eight: 20.3 -> 16.0 us for 2048 rows of
-// 256 tokens in bf16 of 64, 46.9 -> 26.1 in 8 bits of 128; alike for few rows).
+// Whole-row launches: four waves share a row. With eight, 27.5 -> 30.9 us for 2048 rows of
+// 256 tokens in bf16 of 64, 34 -> 50 in 8 bits of 128; 4.3 and 4.3 for 8 rows of 256; 10.2
+// -> 9.3 and 12.1 -> 11.7 for 128 rows of 1024.
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / 64;
 
 // Rows are not shared out where the longest that the table has room for (the
 // lengths themselves are the GPU's) is this short, a CU's intake being 40 to 60 bytes
 // a ns, less in 8 bits. us, whole rows / shared out, 8 rows of four query heads at 256,
-// 384, 512 KB: bf16 of dimension 64 8.2 / 10.2, 10.8 / 10.4, 13.4 / 10.3; of dimension
-// 128 7.9 / 10.8, 10.1 / 11.1, 12.2 / 10.9; fp32 8.9 / 11.7, 11.6 / 11.8, 14.5 / 11.8; 8
-// bits of dimension 128 10.3 / 10.8, 13.4 / 10.8, 16.6 / 10.8; 128 rows at 384 KB 11.3 /
-// 14.6 (bf16, 128), 1024 rows 48.6 / 49.2. Shared out takes a second launch, about 4 us
-// of the host's time.
+// 384, 512 KB: bf16 of dimension 64 8.3 / 9.6, 10.9 / 9.7, 13.4 / 9.7; of dimension 128
+// 7.9 / 10.3, 10.0 / 10.5, 12.2 / 10.5; fp32 8.9 / 11.4, 11.6 / 11.6, 14.3 / 11.4; 8
+// bits of dimension 128 10.3 / 10.2, 13.3 / 10.3, 16.6 / 10.3. With more rows whole ones
+// stay ahead: at 384 KB 11.6 / 16.4 for 128 rows, 74 / 78 for 1024 (bf16, 128), and in 8
+// bits 15.8 / 17.9 and 76 / 81 above the limit; but the same table may hold one long
+// sequence and short ones, which whole rows leave to one CU. Shared out takes a second
+// launch, about 4 us of the host's time.
 constexpr int64_t kWholeRowBytes = 384 << 10, kWholeRowBytes8 = 256 << 10;
 inline bool whole_rows(int dtype, int dim, const DecodeArgs& a) {
   const int size = dtype == 0 ? 4 : dtype == 1 ? 2 : 1;

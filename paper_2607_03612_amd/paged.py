@@ -140,6 +140,7 @@ def _step_workspace(*sizes) -> int:
 
 
 def page_tables_workspace_bytes(requests, page_size, max_pages, pages, tokens, in_place=False) -> int:
+    """Bytes of the workspace of ``page_tables``, 0 for the steps that are one launch."""
     _check_sizes([abs(x) for x in (requests, page_size, max_pages, pages, tokens)])
     r = _step_workspace(requests, page_size, max_pages, pages, tokens, int(in_place))
     binding._check(min(r, 0), "saf3r_page_tables_workspace_bytes")
@@ -275,6 +276,7 @@ def _attention_workspace(code, kv_heads, page_size, head_dim, q_heads, requests,
 
 
 def paged_attention_workspace_bytes(q, k_pages, v_pages, page_table, k_exp=None, v_exp=None) -> int:
+    """Bytes of the workspace of ``paged_attention``, 0 where the table's rows are short."""
     _lib()
     _check_sizes(q.shape, k_pages.shape, page_table.shape)
     c, _ = _layout(k_pages, v_pages, k_exp, v_exp)
