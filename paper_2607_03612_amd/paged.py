@@ -100,11 +100,11 @@ def _check_int(name, x, low):
         raise ValueError(f"{name} must be in [{low}, 2^31)")
 
 
-def _check_sizes(*shapes):
-    """The library takes sizes as int32, and ctypes drops what does not fit."""
-    for shape in shapes:
-        if max(shape, default=0) > _INT_MAX:
-            raise ValueError("sizes must be below 2^31")
+def _check_sizes(together):
+    """The library takes sizes as int32, and ctypes drops what does not fit. `together`:
+    the bits of several."""
+    if together > _INT_MAX:
+        raise ValueError("sizes must be below 2^31")
 
 
 def _check_words(name, t, shape, device):
@@ -141,7 +141,7 @@ def _step_workspace(*sizes) -> int:
 
 def page_tables_workspace_bytes(requests, page_size, max_pages, pages, tokens, in_place=False) -> int:
     """Bytes of the workspace of ``page_tables``, 0 for the steps that are one launch."""
-    _check_sizes([abs(x) for x in (requests, page_size, max_pages, pages, tokens)])
+    _check_sizes(max(abs(x) for x in (requests, page_size, max_pages, pages, tokens)))
     r = _step_workspace(requests, page_size, max_pages, pages, tokens, int(in_place))
     binding._check(min(r, 0), "saf3r_page_tables_workspace_bytes")
     return int(r)
@@ -162,12 +162,12 @@ def page_tables(lengths, new_tokens, free_pages, free_count, page_table, page_si
     lib = _lib()
     _check_int("page_size", page_size, 1)
     _check_int("tokens", tokens, 0)
-    _check_sizes(lengths.shape, free_pages.shape, page_table.shape)
-    dev = lengths.device
-    _check_device(dev)
     if lengths.dim() != 1 or free_pages.dim() != 1 or page_table.dim() != 2:
         raise ValueError("lengths must be [requests], free_pages [pages] and page_table [requests, max_pages]")
     R, width, pages = lengths.shape[0], page_table.shape[1], free_pages.shape[0]
+    _check_sizes(R | width | pages)
+    dev = lengths.device
+    _check_device(dev)
     _check_words("lengths", lengths, (R,), dev)
     _check_words("new_tokens", new_tokens, (R,), dev)
     _check_words("free_pages", free_pages, (pages,), dev)
@@ -216,13 +216,14 @@ def _layout(k_pages, v_pages, k_exp, v_exp):
     if dtype not in _TYPES:
         raise ValueError(f"unsupported cache dtype {dtype}")
     code, kind = _TYPES[dtype]
-    _check_device(dev)
     if len(shape) != 4 or strides[3] != 1:
         raise ValueError("pages must be [pages, kv_heads, page_size, head_dim], head_dim contiguous")
+    n, H, ps, D = shape
+    _check_sizes(n | H | ps | D)
+    _check_device(dev)
     if v_pages.shape != shape or v_pages.dtype != dtype or v_pages.device != dev \
             or (v_pages.stride() != strides and not _same_strides(k_pages, v_pages)):
         raise ValueError("k_pages and v_pages must share shape, strides, dtype and device")
-    n, H, ps, D = shape
     if code == E4M3:
         for t in (k_exp, v_exp):
             if t is None or t.dtype != torch.uint8 or not t.is_contiguous() or t.shape != (n, H, ps) or t.device != dev:
@@ -250,14 +251,16 @@ def cache_append(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=N
     one, the latter with the exponents ``k_exp`` and ``v_exp``. Slots outside the
     cache (-1) are skipped; the others must be distinct."""
     lib = _lib()
-    _check_sizes(k.shape, k_pages.shape)
-    layout, kind = _layout(k_pages, v_pages, k_exp, v_exp)
     dev, shape, strides = k.device, k.shape, k.stride()
-    if k.dtype != kind or dev != k_pages.device or len(shape) != 3 or strides[2] != 1:
+    if len(shape) != 3:
+        raise ValueError("k and v must be [kv_heads, tokens, head_dim]")
+    H, T, D = shape
+    _check_sizes(T)
+    layout, kind = _layout(k_pages, v_pages, k_exp, v_exp)
+    if k.dtype != kind or dev != k_pages.device or strides[2] != 1:
         raise ValueError(f"k and v must be {kind} tensors [kv_heads, tokens, head_dim] on {k_pages.device}, head_dim contiguous")
     if v.shape != shape or v.dtype != kind or v.device != dev or (v.stride() != strides and not _same_strides(k, v)):
         raise ValueError("k and v must share shape, strides, dtype and device")
-    H, T, D = shape
     if H != layout.kv_heads or D != layout.head_dim:
         raise ValueError("k and v must have the cache's kv_heads and head_dim")
     _check_apart("the pages", k_pages)
@@ -278,7 +281,7 @@ def _attention_workspace(code, kv_heads, page_size, head_dim, q_heads, requests,
 def paged_attention_workspace_bytes(q, k_pages, v_pages, page_table, k_exp=None, v_exp=None) -> int:
     """Bytes of the workspace of ``paged_attention``, 0 where the table's rows are short."""
     _lib()
-    _check_sizes(q.shape, k_pages.shape, page_table.shape)
+    _check_sizes(q.shape[0] | q.shape[1] | page_table.shape[1])
     c, _ = _layout(k_pages, v_pages, k_exp, v_exp)
     r = _attention_workspace(c.dtype, c.kv_heads, c.page_size, c.head_dim, q.shape[0], q.shape[1], page_table.shape[1])
     binding._check(min(r, 0), "saf3r_paged_attention_workspace_bytes")
@@ -298,15 +301,15 @@ def paged_attention(q, k_pages, v_pages, page_table, lengths, k_exp=None, v_exp=
     lib = _lib()
     _check_int("anchor", anchor, 0)
     _check_int("window", window, 0)
-    _check_sizes(q.shape, k_pages.shape, page_table.shape)
-    layout, kind = _layout(k_pages, v_pages, k_exp, v_exp)
-    dev, shape, strides = k_pages.device, q.shape, q.stride()
-    if q.dtype != kind or q.device != dev or len(shape) != 3 or strides[2] != 1 or shape[2] != layout.head_dim:
-        raise ValueError(f"q must be a {kind} tensor [q_heads, requests, {layout.head_dim}] on {dev}, head_dim contiguous")
+    dev, shape, strides, table = k_pages.device, q.shape, q.stride(), page_table.shape
+    if len(shape) != 3 or len(table) != 2:
+        raise ValueError("q must be [q_heads, requests, head_dim] and page_table [requests, max_pages]")
     Hq, R, D = shape
-    if page_table.dim() != 2:
-        raise ValueError("page_table must be [requests, max_pages]")
-    width = page_table.shape[1]
+    width = table[1]
+    _check_sizes(Hq | R | width)
+    layout, kind = _layout(k_pages, v_pages, k_exp, v_exp)
+    if q.dtype != kind or q.device != dev or strides[2] != 1 or D != layout.head_dim:
+        raise ValueError(f"q must be a {kind} tensor [q_heads, requests, {layout.head_dim}] on {dev}, head_dim contiguous")
     _check_words("page_table", page_table, (R, width), dev)
     _check_words("lengths", lengths, (R,), dev)
     made = []
