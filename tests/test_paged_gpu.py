@@ -859,3 +859,84 @@ def test_a_call_on_another_stream_waits_for_the_memory_that_it_allocates(gpu_lib
         if got[0].dtype == torch.bfloat16:
             assert torch.equal(got[0], want)
         del busy
+
+
+def test_the_binding_refuses_before_it_writes(gpu_lib):
+    """Tensors on the GPU whose type, shape, place, strides or alignment is off; everything stays as it was."""
+    import paper_2607_03612_amd as P
+
+    bf, f32, D = torch.bfloat16, torch.float32, 64
+    new = lambda *s, dtype=bf: torch.full(s, 3.0, device=DEV).to(dtype)  # noqa: E731
+    kp, vp = new(4, 2, 16, D), new(4, 2, 16, D)
+    k8, v8 = (new(4, 2, 16, D, dtype=torch.float8_e4m3fn) for _ in range(2))
+    e8 = torch.full((4, 2, 16), 127, dtype=torch.uint8, device=DEV)
+    k, slots = new(2, 5, D), ints(range(5))
+    table, lengths, q = ints(np.zeros((3, 2))), ints([1, 2, 3]), new(4, 3, D)
+    out = new(4, 3, D)
+    shifted = new(2 * 5 * D + 1)[1:].view(2, 5, D)
+    append, attend_ = P.cache_append, P.paged_attention
+    for call in (
+        lambda: append(k.float(), k.float(), slots, kp, vp),
+        lambda: append(k, k[:, :4], slots, kp, vp),
+        lambda: append(k, k.transpose(0, 1).contiguous().transpose(0, 1), slots, kp, vp),
+        lambda: append(k, k.cpu(), slots, kp, vp),
+        lambda: append(k[:1], k[:1], slots, kp, vp),
+        lambda: append(k[0], k[0], slots, kp, vp),
+        lambda: append(new(2, 5, 128), new(2, 5, 128), slots, kp, vp),
+        lambda: append(new(2, 5, 2 * D)[:, :, ::2], new(2, 5, 2 * D)[:, :, ::2], slots, kp, vp),
+        lambda: append(shifted, shifted, slots, kp, vp),
+        lambda: append(k, k, slots[:4], kp, vp),
+        lambda: append(k, k, slots.long(), kp, vp),
+        lambda: append(k, k, slots.cpu(), kp, vp),
+        lambda: append(k, k, slots, kp, vp, e8, e8),
+        lambda: append(k, k, slots, k8, v8),
+        lambda: append(k, k, slots, k8, v8, e8, e8[:3]),
+        lambda: append(k, k, slots, k8, v8, e8, e8.int()),
+        lambda: append(k, k, slots, kp, vp[:3]),
+        lambda: append(k, k, slots, kp, vp.transpose(1, 2).contiguous().transpose(1, 2)),
+        lambda: append(k, k, slots, kp[:1].expand(4, 2, 16, D), vp[:1].expand(4, 2, 16, D)),
+        lambda: append(k, k, slots, kp.half(), vp.half()),
+        lambda: append(k, k, slots, kp[:, :, :8], vp[:, :, :8]),
+        lambda: attend_(q.float(), kp, vp, table, lengths),
+        lambda: attend_(q[0], kp, vp, table, lengths),
+        lambda: attend_(new(4, 3, 128), kp, vp, table, lengths),
+        lambda: attend_(q[:3], kp, vp, table, lengths),
+        lambda: attend_(q.cpu(), kp, vp, table, lengths),
+        lambda: attend_(q, kp, vp, table[:2], lengths),
+        lambda: attend_(q, kp, vp, table[0], lengths),
+        lambda: attend_(q, kp, vp, table.t().contiguous().t(), lengths),
+        lambda: attend_(q, kp, vp, table, lengths[:2]),
+        lambda: attend_(q, kp, vp, table, lengths.float()),
+        lambda: attend_(q, kp, vp, table[:, :0], lengths),
+        lambda: attend_(q[:, :0], kp, vp, table[:0], lengths[:0]),
+        lambda: attend_(q, kp, vp, table, lengths, out=out.float()),
+        lambda: attend_(q, kp, vp, table, lengths, out=out[:, :2]),
+        lambda: attend_(q, kp, vp, table, lengths, out=out[:1].expand(4, 3, D)),
+        lambda: attend_(q, kp, vp, table, lengths, out=new(4, 3, 2 * D)[:, :, ::2]),
+        lambda: attend_(q, kp, vp, table, lengths, out=out, scale=0.0),
+        lambda: attend_(q, kp, vp, table, lengths, out=out, scale=math.nan),
+        lambda: attend_(q, kp, vp, ints(np.zeros((3, 400))), lengths, out=out, workspace=new(16)),
+        lambda: attend_(q, kp, vp, table, lengths, out=out, workspace=new(16, 16).t()[1:]),
+        lambda: attend_(q, k8, v8, table, lengths, out=out),
+        lambda: attend_(q, kp, vp, table, lengths, e8, e8, out=out),
+    ):
+        with pytest.raises((ValueError, P.Saf3rError)):
+            call()
+    free, count, grow = ints(range(4)), ints([4]), ints([1, 1, 1])
+    step = lambda **kw: dict(dict(lengths=lengths, new_tokens=grow, free_pages=free, free_count=count, page_table=table,  # noqa: E731
+                                  page_size=16, tokens=3), **kw)
+    for kw in (dict(lengths=lengths.long()), dict(lengths=lengths[:2]), dict(new_tokens=grow[:2]), dict(new_tokens=grow.float()),
+               dict(free_pages=free[::2]), dict(free_pages=free[:0]), dict(free_count=ints([4, 4])), dict(free_count=count.cpu()),
+               dict(page_table=table[:2]), dict(page_table=table.t().contiguous().t()), dict(page_table=table[:, :0]),
+               dict(page_size=24), dict(page_size=2048), dict(lengths_out=lengths.long()), dict(slots=ints(range(4))),
+               dict(token_start=ints(range(3))), dict(free_count_out=count.cpu()), dict(workspace=new(8, 8).t()[1:])):
+        with pytest.raises((ValueError, P.Saf3rError)):
+            P.page_tables(**step(**kw))
+    many = ints(np.zeros(2000))
+    with pytest.raises(P.Saf3rError):
+        P.page_tables(many, many, free, count, ints(np.zeros((2000, 1))), 16, 3, workspace=new(16))
+    torch.cuda.synchronize()
+    for t in (kp, vp, k8, v8, out):
+        assert bool((t.float() == 3).all())
+    assert bool((e8 == 127).all()) and table.count_nonzero() == 0 and lengths.tolist() == [1, 2, 3]
+    assert free.tolist() == [0, 1, 2, 3] and int(count) == 4
