@@ -71,7 +71,7 @@ saf3r_status saf3r_paged_attention_scored(const saf3r_page_layout* cache, const 
  * that saf3r_page_tables refused kept its length: its new tokens count as its last ones, and
  * their rows mean nothing. token_start is read as 0 .. tokens and has to ascend; of a
  * request whose end lies before its start there are no new tokens, and where starts go
- * back, rows are any request's.
+ * back, the rows of out and lse mean nothing.
  * What lies in the cache behind a sequence's end does not reach the output, infinities and
  * NaN included; such values among a request's own keys and values are undefined, those of
  * a query reach its own row only.
