@@ -176,7 +176,7 @@ struct PromptArgs {
   int32_t tiles;      // numbers of tiles of a key-value head, over all requests
   int32_t groups;     // workgroups that the steps are dealt out to; 0: one for each tile
   int32_t slot_rows;  // rows of a part in the workspace
-  int32_t far_cap;    // the cap is over kNearCap
+  int32_t far_cap;    // the cap is over kNearCap, or cap_in * kTwoLog2e is not finite
   float scale_log2;   // scale * log2(e)
   float cap_in, cap_out;  // as in DecodeArgs
   const float* slopes;
@@ -191,6 +191,7 @@ struct PromptArgs {
 constexpr int32_t kTilesAcross = 1 << 15;
 constexpr int32_t kMaxPromptTokens = 1 << 22;  // times 256 query heads: 2^30 rows
 constexpr float kNearCap = 2048.0f;
+constexpr float kTwoLog2e = 2.8853900817779268f;  // e^2y = 2^(kTwoLog2e y)
 // A tile's rows are new tokens times the query heads of a key-value head, a token's heads one
 // after another; 64 (fp32: 32) for each of four waves.
 inline void plan_prompt(int dtype, int dim, PromptArgs* a) {

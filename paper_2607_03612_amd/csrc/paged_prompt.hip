@@ -625,8 +625,9 @@ struct Rows {
   // The cap as cap - 2 cap / (1 + e^2y): five vector instructions' time less than the above, off
   // by 5 2^-24 of the cap. At a cap of 2048 and below that is less than 2^-10, where the weights'
   // own rounding is 2^-8 of each; beyond, scores are changed by the above ahead of the products.
+  // So they are where the factor below would be infinite, and a score of 0 times it no number.
   __device__ __forceinline__ float capped(const PromptArgs& a, float z) const {
-    const float t = __builtin_amdgcn_exp2f(z * (a.cap_in * 2.8853900817779268f));
+    const float t = __builtin_amdgcn_exp2f(z * (a.cap_in * kTwoLog2e));
     return fmaf(-2.0f * a.cap_out, __builtin_amdgcn_rcpf(1.0f + t), a.cap_out);
   }
   __device__ __forceinline__ float far_of(int tq, int32_t base, int hf) const { return (float)(place[tq] - base - 4 * hf); }

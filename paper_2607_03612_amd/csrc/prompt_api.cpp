@@ -41,7 +41,7 @@ saf3r_status check_prompt(const saf3r_page_layout* cache, const saf3r_prompt* p,
   a->token_stride = d.token_stride;
   a->page_stride = d.page_stride;
   a->head_stride = d.head_stride;
-  a->far_cap = p->cap > saf3r::kNearCap;
+  a->far_cap = p->cap > saf3r::kNearCap || !isfinite(a->cap_in * saf3r::kTwoLog2e);
   saf3r::plan_prompt(cache->dtype, cache->head_dim, a);
   return SAF3R_OK;
 }

@@ -3,9 +3,27 @@ import numpy as np
 import pytest
 import torch
 
-from prompt_cases import DEV, Cache, ints, queries, wide
+from oracle import prompt as Q
+from prompt_cases import DEV, TYPES, Cache, check, ints, quantised, queries, wide
 
 pytestmark = pytest.mark.gpu
+
+ALL = ["f32", "bf16", "e4m3", "e2m1"]
+
+
+def held(dtype, k, v, ps=16):
+    """One sequence of the tokens ``k``, ``v [n, kv_heads, dim]`` in a cache: pages, exponents, table, and what it keeps of them."""
+    import paper_2607_03612_amd as P
+
+    n, H, D = k.shape
+    pages = -(-n // ps)
+    raw = torch.uint8 if dtype in ("e4m3", "e2m1") else TYPES[dtype]
+    kv = [torch.zeros((pages, H, ps, D // 2 if dtype == "e2m1" else D), dtype=raw, device=DEV).view(TYPES[dtype]) for _ in range(2)]
+    shape = (pages, H, ps, D // 32) if dtype == "e2m1" else (pages, H, ps)
+    exps = [torch.zeros(shape, dtype=torch.uint8, device=DEV) if raw == torch.uint8 else None for _ in range(2)]
+    rows = [torch.from_numpy(np.ascontiguousarray(x.transpose(1, 0, 2))).to(DEV).to(wide(dtype)) for x in (k, v)]
+    P.cache_append(*rows, ints(np.arange(n)), *kv, *exps)
+    return kv, exps, ints(np.arange(pages)[None]), quantised(k, dtype)[0], quantised(v, dtype)[0]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32", "e2m1"])
@@ -38,3 +56,25 @@ def test_starts_that_go_back_over_long_sequences(gpu_lib, dtype):
         assert bool((out[:32] == 7).all()) and bool((out[T + 32:] == 7).all())
     got, lse = run(right)
     assert torch.equal(got[:, :3584], want[:, :3584]) and torch.equal(lse[:, :3584], want_lse[:, :3584])
+
+
+@pytest.mark.parametrize("dtype", ALL)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("scale,cap", [(2.0 ** 124, 0.125), (0.125, 1e-39), (0.5, 2.0 ** -126)])
+def test_a_scale_that_is_large_for_its_cap(gpu_lib, dtype, D, scale, cap):
+    """scale / cap near the largest number: keys at right angles to the query have a score of 0, others one of the cap's
+    size, in steps that a mask crosses and in those that it does not."""
+    import paper_2607_03612_amd as P
+
+    n, T = 600, 70
+    rng = np.random.default_rng(D)
+    k = np.repeat((np.arange(n) % 3 - 1.0)[:, None, None], D, 2)
+    k[200:330] = 0  # whole steps of nothing but 0
+    kv, exps, table, k, v = held(dtype, k, rng.standard_normal((n, 1, D)))
+    q = torch.full((2, T, D), 2.0 ** -10, dtype=wide(dtype), device=DEV)
+    q[1, 3] = 0
+    out, lse = P.prompt_attention(q, *kv, table, ints([n]), ints([0, T]), *exps, scale=scale, cap=cap, want_lse=True)
+    place = np.arange(n - T, n)
+    # tanh is 0 or +-1: so it is at 40 for the oracle, whose bounds then are those of scores of the cap's size
+    want = Q.attend(q.double().cpu().numpy(), place, k, v, 40 * cap / (D * 2.0 ** -10), Q.seen(n, place), cap)
+    check(out, lse, want, dtype, 0 if dtype == "f32" else 8, n)
