@@ -75,6 +75,7 @@ saf3r_status saf3r_paged_attention_scored(const saf3r_page_layout* cache, const 
  * What lies in the cache behind a sequence's end does not reach the output, infinities and
  * NaN included; such values among a request's own keys and values are undefined, those of
  * a query reach its own row only.
+ * Scores of any size are taken, as fp32 holds them: scale * log2(e) * q . k has to be finite.
  * fp32 caches: fp32 products. The others: exact bf16 operands with fp32 accumulation,
  * softmax and sums in fp32, the weights rounded to bf16 (2^-8) for the product with V.
  * Same inputs, same bits.

@@ -569,6 +569,7 @@ struct Rows {
   bf16x8 q[2][kS];      // Q^T as the B operand: dimensions 16 s + 8 hf .. of row 32 tq + l32
   f32x16 o[kC][2];      // register e: dimension 32 c + 8 (e / 4) + 4 hf + e % 4
   float nm[2], l[2];    // minus the running maximum (log2), this lane's share of the sum
+  uint64_t far = 0;     // the lanes with a far maximum
   float slope[2];       // of the row's head
   int32_t place[2];     // changed scores: the row's place
   // Lane parts of LDS addresses, of a panel. An empty asm defines them anew at each use, so
@@ -654,15 +655,23 @@ struct Rows {
     sum += y;
     return bf16x2{(__bf16)x, (__bf16)y};
   }
+  // From a maximum of 2^24 on its rounding is a power of two and more, as much as that of the scores
+  // themselves: they are scaled first, so that the largest one's weight is 1.
+  __device__ __forceinline__ static bool is_far(float nm) { return kScored == 0 && fabsf(nm) >= 16777216.0f; }
   __device__ __forceinline__ void weights(const f32x16 (&z)[2], const float (&nmu)[2], float sc, bf16x8 (&p)[2][2], float (&sum)[2]) const {
 #pragma unroll
     for (int tq = 0; tq < 2; ++tq) {
       sum[tq] = 0.0f;
+      const bool far = is_far(nmu[tq]);
+      const float by = far ? sc : 1.0f, then = far ? 1.0f : sc;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         bf16x2 x[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = pair(z[tq][8 * u + 2 * e], z[tq][8 * u + 2 * e + 1], sc, nmu[tq], sum[tq]);
+        for (int e = 0; e < 4; ++e) {
+          const int i = 8 * u + 2 * e;
+          x[e] = pair(kScored ? z[tq][i] : z[tq][i] * by, kScored ? z[tq][i + 1] : z[tq][i + 1] * by, kScored ? sc : then, nmu[tq], sum[tq]);
+        }
         p[u][tq] = bf16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
       }
     }
@@ -764,9 +773,10 @@ struct Rows {
   // The maximum moves only where a row's sum leaves [0, 2^12]: at its first key, where the
   // maximum is still none and the sum infinite or NaN, and where scores grew by much. A
   // row without a key so far keeps m = -inf and weights of 0; a row whose sum is in order
-  // keeps its maximum, whatever the others of the wave do.
+  // keeps its maximum, whatever the others of the wave do. Weights below a far maximum are
+  // always taken again.
   __device__ __forceinline__ void settle(const f32x16 (&z)[2], float sc, bf16x8 (&p)[2][2], float (&sum)[2]) {
-    if (__ballot(__float_as_uint(sum[0]) > 0x45800000u || __float_as_uint(sum[1]) > 0x45800000u)) {
+    if (__ballot(__float_as_uint(sum[0]) > 0x45800000u || __float_as_uint(sum[1]) > 0x45800000u) | far) {
       float use[2];
 #pragma unroll
       for (int tq = 0; tq < 2; ++tq) {
@@ -784,6 +794,7 @@ struct Rows {
 #pragma unroll
         for (int c = 0; c < kC; ++c) o[c][tq] *= f;
       }
+      far = __ballot(is_far(nm[0]) || is_far(nm[1]));
       weights(z, use, sc, p, sum);
     }
     l[0] += sum[0];

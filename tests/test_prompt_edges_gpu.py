@@ -78,3 +78,57 @@ def test_a_scale_that_is_large_for_its_cap(gpu_lib, dtype, D, scale, cap):
     # tanh is 0 or +-1: so it is at 40 for the oracle, whose bounds then are those of scores of the cap's size
     want = Q.attend(q.double().cpu().numpy(), place, k, v, 40 * cap / (D * 2.0 ** -10), Q.seen(n, place), cap)
     check(out, lse, want, dtype, 0 if dtype == "f32" else 8, n)
+
+
+def far_scores(D, n, seed=0):
+    """Keys of one value each, 3 2^(e - 1) or 2^e with e rising by one every 40 keys: exact in every type."""
+    g = np.arange(n) // 20
+    k = np.repeat((2.0 ** (10 + g // 2) * np.where(g % 2, 1.5, 1.0))[:, None, None], D, 2)
+    return k, np.random.default_rng(seed).standard_normal((n, 1, D))
+
+
+def far_want(q_value, k, v, D, scale, keep):
+    """Scores that far apart leave the keys of the largest one, in equal parts; each score is off by (D + 8) u of its size."""
+    z = scale * q_value * D * k[:, 0, 0]
+    z = np.where(keep, z, -np.inf)
+    top = z.max(1, keepdims=True)
+    w = (z == top) / (z == top).sum(1, keepdims=True)
+    out = w @ v[:, 0]
+    lse = top[:, 0] + np.log((z == top).sum(1))
+    return (out[None], lse[None], (D + 8) * 2.0 ** -24 * np.abs(top[None, :, 0]), np.zeros_like(out[None]),
+            (w @ np.abs(v[:, 0]) + np.abs(out))[None])
+
+
+@pytest.mark.parametrize("dtype", ALL)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("q_value", [2.0 ** 2, 2.0 ** 8, 2.0 ** 13, 1.5 * 2.0 ** 15, -2.0 ** 16, 2.0 ** 40, -2.0 ** 60])
+def test_far_scores(gpu_lib, dtype, D, q_value):
+    """Scores from 1e5 on, up to 1e25: what is left of a product's rounding behind the maximum is more than an exponent
+    holds. A single key, growing ones, and a split along the keys."""
+    import paper_2607_03612_amd as P
+
+    for n, T in ((1, 1), (3, 2), (170, 70), (290, 290)):
+        k, v = far_scores(D, n)
+        kv, exps, table, k, v = held(dtype, k, v)
+        q = torch.full((1, T, D), q_value, dtype=wide(dtype), device=DEV)
+        out, lse = P.prompt_attention(q, *kv, table, ints([n]), ints([0, T]), *exps, want_lse=True)
+        keep = Q.seen(n, np.arange(n - T, n))
+        check(out, lse, far_want(q_value, k, v, D, D ** -0.5, keep), dtype, 0 if dtype == "f32" else 8, n)
+
+
+def test_far_scores_leave_other_rows(gpu_lib):
+    """A row whose scores are far changes no bit of its neighbours'."""
+    import paper_2607_03612_amd as P
+
+    c = Cache(3, "bf16", [700], 2, 64, 16)
+    q = queries(4, 8, 100, 64, "bf16")
+    want, want_lse = P.prompt_attention(q, *c.kv, c.table, c.lengths, ints([0, 100]), want_lse=True)
+    q[2, 40] *= 2.0 ** 40
+    q[7, 99] *= 2.0 ** 30
+    out, lse = P.prompt_attention(q, *c.kv, c.table, c.lengths, ints([0, 100]), want_lse=True)
+    for h, t in ((2, 40), (7, 99)):
+        top = (q[h, t].double().cpu().numpy() @ c.tokens["k"][0][: 601 + t, h // 4].T).argmax()
+        v = c.tokens["v"][0][top, h // 4]
+        assert np.all(np.abs(out[h, t].double().cpu().numpy() - v) <= 2.0 ** -7 * np.abs(v)) and bool(lse[h, t].isfinite())
+        out[h, t], lse[h, t] = want[h, t], want_lse[h, t]
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
