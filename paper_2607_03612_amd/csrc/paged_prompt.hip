@@ -562,6 +562,10 @@ struct Limits {
   int32_t place, below, from;
 };
 
+// A weight is 2^(z scale - m) with the product unrounded and m its rounded maximum: from here on
+// the rounding is a power of two and more, as much as that of the scores themselves.
+constexpr float kFarMaximum = 16777216.0f;
+
 // kScored: 0 as they are, 1 lowered by the distance, 2 capped (and lowered).
 template <int kDim, int kScored>
 struct Rows {
@@ -569,7 +573,6 @@ struct Rows {
   bf16x8 q[2][kS];      // Q^T as the B operand: dimensions 16 s + 8 hf .. of row 32 tq + l32
   f32x16 o[kC][2];      // register e: dimension 32 c + 8 (e / 4) + 4 hf + e % 4
   float nm[2], l[2];    // minus the running maximum (log2), this lane's share of the sum
-  uint64_t far = 0;     // the lanes with a far maximum
   float slope[2];       // of the row's head
   int32_t place[2];     // changed scores: the row's place
   // Lane parts of LDS addresses, of a panel. An empty asm defines them anew at each use, so
@@ -655,22 +658,21 @@ struct Rows {
     sum += y;
     return bf16x2{(__bf16)x, (__bf16)y};
   }
-  // From a maximum of 2^24 on its rounding is a power of two and more, as much as that of the scores
-  // themselves: they are scaled first, so that the largest one's weight is 1.
-  __device__ __forceinline__ static bool is_far(float nm) { return kScored == 0 && fabsf(nm) >= 16777216.0f; }
+  // kFar: from a maximum of 2^24 on scores are scaled first, so that the largest one's weight is 1.
+  template <bool kFar>
   __device__ __forceinline__ void weights(const f32x16 (&z)[2], const float (&nmu)[2], float sc, bf16x8 (&p)[2][2], float (&sum)[2]) const {
 #pragma unroll
     for (int tq = 0; tq < 2; ++tq) {
       sum[tq] = 0.0f;
-      const bool far = is_far(nmu[tq]);
+      const bool far = kFar && fabsf(nmu[tq]) >= kFarMaximum;
       const float by = far ? sc : 1.0f, then = far ? 1.0f : sc;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         bf16x2 x[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int i = 8 * u + 2 * e;
-          x[e] = pair(kScored ? z[tq][i] : z[tq][i] * by, kScored ? z[tq][i + 1] : z[tq][i + 1] * by, kScored ? sc : then, nmu[tq], sum[tq]);
+          const float z0 = z[tq][8 * u + 2 * e], z1 = z[tq][8 * u + 2 * e + 1];
+          x[e] = pair(kFar ? z0 * by : z0, kFar ? z1 * by : z1, kFar ? then : sc, nmu[tq], sum[tq]);
         }
         p[u][tq] = bf16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
       }
@@ -773,10 +775,10 @@ struct Rows {
   // The maximum moves only where a row's sum leaves [0, 2^12]: at its first key, where the
   // maximum is still none and the sum infinite or NaN, and where scores grew by much. A
   // row without a key so far keeps m = -inf and weights of 0; a row whose sum is in order
-  // keeps its maximum, whatever the others of the wave do. Weights below a far maximum are
-  // always taken again.
+  // keeps its maximum, whatever the others of the wave do.
+  template <bool kFar = false>
   __device__ __forceinline__ void settle(const f32x16 (&z)[2], float sc, bf16x8 (&p)[2][2], float (&sum)[2]) {
-    if (__ballot(__float_as_uint(sum[0]) > 0x45800000u || __float_as_uint(sum[1]) > 0x45800000u) | far) {
+    if (__ballot(__float_as_uint(sum[0]) > 0x45800000u || __float_as_uint(sum[1]) > 0x45800000u)) {
       float use[2];
 #pragma unroll
       for (int tq = 0; tq < 2; ++tq) {
@@ -794,11 +796,36 @@ struct Rows {
 #pragma unroll
         for (int c = 0; c < kC; ++c) o[c][tq] *= f;
       }
-      far = __ballot(is_far(nm[0]) || is_far(nm[1]));
-      weights(z, use, sc, p, sum);
+      weights<kFar>(z, use, sc, p, sum);
     }
     l[0] += sum[0];
     l[1] += sum[1];
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int tq = 0; tq < 2; ++tq) {
+      nm[tq] = INFINITY;
+      l[tq] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[c][tq][e] = 0.0f;
+    }
+  }
+  // Whether a row's weights may have left the exponent's range: its maximum is far, or was and
+  // left sums that are no numbers. A row without a key has neither.
+  __device__ __forceinline__ bool lost() const {
+    bool y = false;
+#pragma unroll
+    for (int tq = 0; tq < 2; ++tq) {
+      float none = l[tq] * 0.0f;
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) none = fmaf(o[c][tq][e], 0.0f, none);
+      y |= none != 0.0f || (fabsf(nm[tq]) >= kFarMaximum && nm[tq] < INFINITY);
+    }
+    return y;
   }
 };
 
@@ -845,13 +872,8 @@ prompt_bf16_kernel(const char* __restrict__ q, const char* __restrict__ k, const
     const char* from = q + (head * b.q_head + row.token * b.q_token) * 2;
 #pragma unroll
     for (int s = 0; s < w.kS; ++s) w.q[tq][s] = *reinterpret_cast<const bf16x8*>(from + 32 * s + 16 * hf);
-    w.nm[tq] = INFINITY;
-    w.l[tq] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < w.kC; ++c)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) w.o[c][tq][e] = 0.0f;
   }
+  w.clear();
   const int tr_row = 4 * hf + ((lane & 15) >> 2), tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
   for (int s = 0; s < 4; ++s) w.kpart[s] = swz(l32, 2 * s + hf);
@@ -1086,6 +1108,36 @@ prompt_bf16_kernel(const char* __restrict__ q, const char* __restrict__ k, const
     bf16x8 vw[2][W::kC];
     w.read_v(rest == 0 ? vring[3] : rest == 1 ? vring[0] : rest == 2 ? vring[1] : vring[2], vw);
     w.mfma_pv(vw, p);
+  }
+  // Scores that large are for the plainest walk, one step after the other; rows whose scores are
+  // not get the same bits again. (Told apart in each step's settle: 827 -> 855 us for 8 frames.)
+  if constexpr (kScored == 0) {
+    if (__syncthreads_or(w.lost())) {
+      w.clear();
+      for (int32_t x = lo; x < hi; ++x) {
+        const Y y = locate(x);
+        __syncthreads();
+        if constexpr (kType == 1) {
+          dma(k, y, kring[0]);
+          dma(v, y, vring[0]);
+        } else {
+          R r;
+          fetch_both(y, y, r);
+          put(r.k, r.ke, kring[0]);
+          put(r.v, r.ve, vring[0]);
+        }
+        sync(std::true_type{});
+        bf16x8 kw[W::kS], vw[2][W::kC];
+        w.read_k(kring[0], kw);
+        w.mfma_s(kw, z);
+        w.mask(z, y.base, lane, y.absent, limits + wave * 64);
+        float sum[2];
+        w.template weights<true>(z, w.nm, sc, p, sum);
+        w.template settle<true>(z, sc, p, sum);
+        w.read_v(vring[0], vw);
+        w.mfma_pv(vw, p);
+      }
+    }
   }
 
 #pragma unroll
