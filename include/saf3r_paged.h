@@ -175,6 +175,7 @@ saf3r_status saf3r_cache_append(const saf3r_page_layout* cache, const saf3r_toke
  * whose scores are all -inf. What lies in the cache behind a sequence's end or
  * outside its window does not reach the output, infinities and NaN included.
  * Infinite or NaN values among a request's own keys and values are undefined.
+ * Scores of any size are taken, as fp32 holds them: scale * log2(e) * q . k has to be finite.
  * QK^T and PV run on the matrix cores with fp32 accumulation, softmax and sums in
  * fp32. fp32 caches: fp32 products. The others: exact bf16 operands,
  * the weights as two bf16 parts each (16 bits), so that the output's error is

@@ -394,13 +394,22 @@ __device__ inline void add_tile(const DecodeArgs& a, const Place<Shape<kType, kD
   }
   const float m = st.m == -INFINITY ? 0.0f : st.m;  // every score so far -inf: weights 2^-inf = 0
   float p[S::kGroups][4];
+  const auto weights = [&](float by, float then) {
 #pragma unroll
-  for (int u = 0; u < S::kGroups; ++u)
+    for (int u = 0; u < S::kGroups; ++u)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      p[u][r] = exp2_fast(fmaf(z[u][r], scale_log2, -m));
-      st.l += p[u][r];
-    }
+      for (int r = 0; r < 4; ++r) {
+        p[u][r] = exp2_fast(fmaf(z[u][r] * by, then, -m));
+        st.l += p[u][r];
+      }
+  };
+  // From a maximum of 2^24 on its rounding is a power of two and more, as much as that of the
+  // scores themselves: they are scaled first, so that the largest one's weight is 1.
+  const bool far = !kScored && fabsf(m) >= 16777216.0f;
+  if (__any(far))
+    weights(far ? scale_log2 : 1.0f, far ? 1.0f : scale_log2);
+  else
+    weights(1.0f, scale_log2);
   if constexpr (kType == 0) {
 #pragma unroll
     for (int u = 0; u < S::kGroups; ++u)

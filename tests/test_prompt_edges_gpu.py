@@ -1,4 +1,4 @@
-"""Attention of several new tokens per request at the ends of what its arguments may be, on the GPU."""
+"""Attention of one and of several new tokens per request at the ends of what its arguments may be, on the GPU."""
 import numpy as np
 import pytest
 import torch
@@ -114,6 +114,49 @@ def test_far_scores(gpu_lib, dtype, D, q_value):
         out, lse = P.prompt_attention(q, *kv, table, ints([n]), ints([0, T]), *exps, want_lse=True)
         keep = Q.seen(n, np.arange(n - T, n))
         check(out, lse, far_want(q_value, k, v, D, D ** -0.5, keep), dtype, 0 if dtype == "f32" else 8, n)
+
+
+@pytest.mark.parametrize("dtype", ALL)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("q_value", [2.0 ** 2, 2.0 ** 8, 2.0 ** 13, 1.5 * 2.0 ** 15, -2.0 ** 16, 2.0 ** 40, -2.0 ** 60])
+def test_far_scores_of_one_token(gpu_lib, dtype, D, q_value):
+    """The same of one token per request: rows whole and shared out, beside a head whose scores are small."""
+    import paper_2607_03612_amd as P
+
+    for n in (1, 3, 170, 290):
+        k, v = far_scores(D, n)
+        kv, exps, table, k, v = held(dtype, k, v)
+        q = torch.full((2, 1, D), q_value, dtype=wide(dtype), device=DEV)
+        q[1] = 2.0 ** -14
+        keep = np.ones((1, n), dtype=bool)
+        near = Q.attend(q[1:].double().cpu().numpy(), [n - 1], k, v, D ** -0.5, keep)
+        for width in (table.shape[1], 3000):
+            wider = torch.zeros((1, width), dtype=torch.int32, device=DEV)
+            wider[:, :table.shape[1]] = table
+            out, lse = P.paged_attention(q, *kv, wider, ints([n]), *exps, want_lse=True)
+            check(out[:1], lse[:1], far_want(q_value, k, v, D, D ** -0.5, keep), dtype, 0 if dtype == "f32" else 16, n)
+            check(out[1:], lse[1:], near, dtype, 0 if dtype == "f32" else 16, n)
+
+
+@pytest.mark.parametrize("dtype", ALL)
+@pytest.mark.parametrize("q_value", [-2.0 ** 15, -1.5 * 2.0 ** 17, -2.0 ** 40])
+def test_far_scores_that_end_near(gpu_lib, dtype, q_value):
+    """Scores far below 0, with values of 2^100, ahead of some of 0: nothing of the former is left."""
+    import paper_2607_03612_amd as P
+
+    n, T, D = 340, 70, 64
+    k, v = far_scores(D, n)
+    k[n - T:] = 0
+    v[:n - T] *= 2.0 ** 100
+    kv, exps, table, k, v = held(dtype, k, v)
+    q = torch.full((1, T, D), q_value, dtype=wide(dtype), device=DEV)
+    keep = Q.seen(n, np.arange(n - T, n))
+    want = far_want(q_value, k, v, D, D ** -0.5, keep)
+    assert np.allclose(want[1][0], np.log(np.arange(1, T + 1)))
+    out, lse = P.prompt_attention(q, *kv, table, ints([n]), ints([0, T]), *exps, want_lse=True)
+    check(out, lse, want, dtype, 0 if dtype == "f32" else 8, n)
+    out, lse = P.paged_attention(q[:, T - 1:], *kv, table, ints([n]), *exps, want_lse=True)
+    check(out, lse, tuple(x[:, -1:] for x in want), dtype, 0 if dtype == "f32" else 16, n)
 
 
 def test_far_scores_leave_other_rows(gpu_lib):
