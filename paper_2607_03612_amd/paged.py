@@ -78,7 +78,9 @@ def _lib():
 
         torch = module
         _TYPES.update({torch.float32: (binding.F32, torch.float32), torch.bfloat16: (binding.BF16, torch.bfloat16),
-                       torch.float8_e4m3fn: (E4M3, torch.bfloat16), torch.float4_e2m1fn_x2: (E2M1, torch.bfloat16)})
+                       torch.float8_e4m3fn: (E4M3, torch.bfloat16)})
+        if hasattr(torch, "float4_e2m1fn_x2"):
+            _TYPES[torch.float4_e2m1fn_x2] = (E2M1, torch.bfloat16)
         _LIB = _declare(binding.load())
     return _LIB
 
