@@ -28,7 +28,7 @@ extern "C" {
 
 /* The way back of saf3r_cache_append: the values that the slots hold. Token t's rows of
  * head h go to h * head_stride + t * token_stride elements of k and v (strides > 0 along
- * more than one entry, multiples of 16 bytes, no two rows in one place). A slot outside
+ * more than one entry, multiples of 16 bytes, no two rows in one place, be they of k or v). A slot outside
  * [0, pages * page_size) gives zeros; slots may repeat. bf16 is exact for what an 8-bit
  * or 4-bit cache holds (from 2^-126 on; an E2M1 block of exponent 255 is NaN).
  *   slots          int32 [tokens]

@@ -46,11 +46,29 @@ def _lib():
     return _LIB
 
 
+def _within(gap, dims, dim) -> bool:
+    """Whether two rows of ``dim`` entries, each at a multiple of every stride of ``dims`` from its tensor's start, share
+    one, the starts lying ``gap`` apart."""
+    if not dims:
+        return abs(gap) < dim
+    (stride, n), rest = dims[0], dims[1:]
+    reach = sum(s * (m - 1) for s, m in rest) + dim - 1
+    least, most = max(1 - n, -((reach - gap) // stride)), min(n - 1, (gap + reach) // stride)
+    return any(_within(gap - x * stride, rest, dim) for x in range(least, most + 1))
+
+
+def _meet(a, b) -> bool:
+    """Whether two tensors ``[heads, tokens, dim]`` of the same strides, dim contiguous, share an entry."""
+    dims = sorted(((s, n) for s, n in zip(a.stride()[:2], a.shape[:2]) if n > 1), reverse=True)
+    return a.numel() > 0 and _within((b.data_ptr() - a.data_ptr()) // a.element_size(), dims, a.shape[2])
+
+
 def cache_read(slots, k_pages, v_pages, k_exp=None, v_exp=None, k=None, v=None, stream=None):
     """The tokens that ``slots [tokens]`` hold: ``(k, v)``, each ``[kv_heads, tokens,
     head_dim]``, fp32 of an fp32 cache and bf16 of the others, which hold nothing that
     bf16 does not. Zeros for slots outside the cache (-1); slots may repeat. ``k`` and
-    ``v``, where they are passed, have head_dim contiguous and the same strides."""
+    ``v``, where they are passed, have head_dim contiguous, the same strides and no memory
+    in common."""
     lib = _lib()
     layout, kind = paged._layout(k_pages, v_pages, k_exp, v_exp)
     dev = k_pages.device
@@ -72,6 +90,8 @@ def cache_read(slots, k_pages, v_pages, k_exp=None, v_exp=None, k=None, v=None, 
     if k.stride() != v.stride() and not paged._same_strides(k, v):
         raise ValueError("k and v must have the same strides")
     paged._check_apart("k and v", k)
+    if not made and _meet(k, v):
+        raise ValueError("k and v must not share memory")
     rows = TokenLayout(T, 0, k.stride(0), k.stride(1))
     if stream is not None:
         paged._allocated(stream, dev, made)

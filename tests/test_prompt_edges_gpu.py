@@ -175,3 +175,26 @@ def test_far_scores_leave_other_rows(gpu_lib):
         assert np.all(np.abs(out[h, t].double().cpu().numpy() - v) <= 2.0 ** -7 * np.abs(v)) and bool(lse[h, t].isfinite())
         out[h, t], lse[h, t] = want[h, t], want_lse[h, t]
     assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("dtype", ALL)
+def test_read_refuses_rows_in_one_place(gpu_lib, dtype):
+    """k and v in one buffer: side by side they are read, on one another refused."""
+    import paper_2607_03612_amd as P
+
+    c = Cache(5, dtype, [40], 3, 64, 16)
+    slots = ints(np.concatenate([c.table[0, i].item() * 16 + np.arange(16) for i in range(3)])[:40])
+    want = P.cache_read(slots, *c.kv, *c.exps)
+    for shape, take in (((2, 3, 40, 64), lambda t, i: t[i]), ((3, 2, 40, 64), lambda t, i: t[:, i]), ((40, 3, 2, 64), lambda t, i: t[:, :, i].transpose(0, 1)),
+                        ((3, 40, 2, 64), lambda t, i: t[:, :, i])):
+        both = torch.full(shape, 7.0, dtype=wide(dtype), device=DEV)
+        k, v = take(both, 0), take(both, 1)
+        P.cache_read(slots, *c.kv, *c.exps, k=k, v=v)
+        assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+    buffer = torch.full((4, 41, 64), 7.0, dtype=wide(dtype), device=DEV)
+    for k, v in ((buffer[:3, :40], buffer[:3, :40]), (buffer[:3, :40], buffer[:3, 1:]), (buffer[:3, 1:], buffer[1:, :40]),
+                 (buffer[1:, :40], buffer[:3, :40])):
+        with pytest.raises(ValueError, match="share"):
+            P.cache_read(slots, *c.kv, *c.exps, k=k, v=v)
+    torch.cuda.synchronize()
+    assert bool((buffer == 7).all())
