@@ -102,6 +102,12 @@ def _check_int(name, x, low):
         raise ValueError(f"{name} must be in [{low}, 2^31)")
 
 
+def _check_cap(cap):
+    """The library takes it as fp32, and 0 there as none."""
+    if cap != 0 and ctypes.c_float(cap).value == 0:
+        raise ValueError("cap must be 0 or at least fp32's least number")
+
+
 def _check_sizes(together):
     """The library takes sizes as int32, and ctypes drops what does not fit. `together`:
     the bits of several."""
@@ -320,6 +326,7 @@ def paged_attention(q, k_pages, v_pages, page_table, lengths, k_exp=None, v_exp=
     lib = _lib()
     _check_int("anchor", anchor, 0)
     _check_int("window", window, 0)
+    _check_cap(cap)
     dev, shape, strides, table = k_pages.device, q.shape, q.stride(), page_table.shape
     if len(shape) != 3 or len(table) != 2:
         raise ValueError("q must be [q_heads, requests, head_dim] and page_table [requests, max_pages]")

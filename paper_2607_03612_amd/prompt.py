@@ -138,6 +138,7 @@ def prompt_attention(q, k_pages, v_pages, page_table, lengths, token_start, k_ex
     torch = paged.torch
     paged._check_int("anchor", anchor, 0)
     paged._check_int("window", window, 0)
+    paged._check_cap(cap)
     dev, shape, strides, table = k_pages.device, q.shape, q.stride(), page_table.shape
     if len(shape) != 3 or len(table) != 2:
         raise ValueError("q must be [q_heads, tokens, head_dim] and page_table [requests, max_pages]")

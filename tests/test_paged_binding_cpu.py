@@ -62,3 +62,16 @@ def test_shared_entries_are_found(paged):
     dims = [(1 << 33, 256), (128, 1 << 26)]  # the largest sizes, 2^42 entries in all
     assert prompt._within((5 << 33) + 128 * 77 + 127, dims, 128) and not prompt._within((256 << 33) + 5, dims, 128)
     assert not prompt._within((1 << 33) - 128, dims[:1] + [(256, 1 << 24)], 128)
+
+
+@pytest.mark.parametrize("cap", [1e-46, -1e-46, 1e-300, 5e-324])
+def test_a_cap_below_fp32(paged, cap):
+    """The library takes it as fp32, where it would be 0: no cap."""
+    from paper_2607_03612_amd import prompt
+
+    pages, q = torch.zeros((3, 2, 16, 64), dtype=torch.bfloat16), torch.zeros((2, 1, 64), dtype=torch.bfloat16)
+    words = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError, match="cap"):
+        paged.paged_attention(q, pages, pages, words(1, 2), words(1), cap=cap)
+    with pytest.raises(ValueError, match="cap"):
+        prompt.prompt_attention(q, pages, pages, words(1, 2), words(1), words(2), cap=cap)
