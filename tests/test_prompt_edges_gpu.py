@@ -5,6 +5,7 @@ import torch
 
 from oracle import prompt as Q
 from prompt_cases import DEV, TYPES, Cache, check, ints, quantised, queries, wide
+from test_scores_gpu import slopes_of
 
 pytestmark = pytest.mark.gpu
 
@@ -198,3 +199,29 @@ def test_read_refuses_rows_in_one_place(gpu_lib, dtype):
             P.cache_read(slots, *c.kv, *c.exps, k=k, v=v)
     torch.cuda.synchronize()
     assert bool((buffer == 7).all())
+
+
+@pytest.mark.parametrize("dtype", ALL)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap", [1900.0, 2048.0, 2048.0 * (1 + 2.0 ** -23), 1e5, 1e9])
+@pytest.mark.parametrize("size,kind", [(0.02, None), (4.0, None), (0.02, "falling"), (4.0, "falling")])
+def test_large_caps(gpu_lib, dtype, D, cap, size, kind):
+    """Up to a cap of 2048 a score is off by 5 2^-24 of the cap; beyond by a few roundings of its own, however large the
+    cap: tanh's argument and result, both constants and the product, 6 u of the score, less than a tenth of what its sum
+    of products may be off by. Steps with and without a mask, and a prefix that all see."""
+    import paper_2607_03612_amd as P
+
+    n, T = 700, 80
+    c = Cache(6, dtype, [n], 2, D, 16)
+    q = queries(7, 4, T, D, dtype, scale=size)
+    slopes = None if kind is None else slopes_of(4, kind)
+    out, lse = P.prompt_attention(q, *c.kv, c.table, c.lengths, ints([0, T]), *c.exps, prefix=ints([650]), cap=cap, slopes=slopes,
+                                  want_lse=True)
+    place = np.arange(n - T, n)
+    args = (q.double().cpu().numpy(), place, c.tokens["k"][0], c.tokens["v"][0], D ** -0.5, Q.seen(n, place, 650))
+    slopes = None if kind is None else slopes.double().cpu().numpy()
+    want = Q.attend(*args, cap, slopes)
+    if cap > 2048:
+        uncapped = Q.attend(*args, 0.0, slopes)
+        want = (*want[:2], 1.1 * uncapped[2], 1.1 * uncapped[3], want[4])
+    check(out, lse, want, dtype, 0 if dtype == "f32" else 8, n)
