@@ -192,6 +192,9 @@ constexpr int32_t kTilesAcross = 1 << 15;
 constexpr int32_t kMaxPromptTokens = 1 << 22;  // times 256 query heads: 2^30 rows
 constexpr float kNearCap = 2048.0f;
 constexpr float kTwoLog2e = 2.8853900817779268f;  // e^2y = 2^(kTwoLog2e y)
+constexpr int32_t kMaxGroups = 512;  // that steps are dealt out to
+// A launch that deals them out has fewer tiles than two turns, and of requests no more than tiles.
+constexpr int32_t kMaxDealt = 2 * kMaxGroups;
 // A tile's rows are new tokens times the query heads of a key-value head, a token's heads one
 // after another; 64 (fp32: 32) for each of four waves.
 inline void plan_prompt(int dtype, int dim, PromptArgs* a) {
@@ -199,7 +202,7 @@ inline void plan_prompt(int dtype, int dim, PromptArgs* a) {
   a->tile_rows = dtype == 0 ? 128 : 256;
   a->tiles = (int32_t)(rows / a->tile_rows + a->requests);
   // as many as run at once, by the registers
-  const int groups = dim == 128 && dtype != 0 ? 256 : 512;
+  const int groups = dim == 128 && dtype != 0 ? 256 : kMaxGroups;
   // with two turns of them and more a workgroup for each tile
   a->groups = rows == 0 || (int64_t)a->tiles * a->kv_heads >= 2 * groups ? 0 : groups;
   a->slot_rows = rows < a->tile_rows ? (int32_t)rows : a->tile_rows;

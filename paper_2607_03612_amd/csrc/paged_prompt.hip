@@ -110,7 +110,7 @@ struct Run {
   bool nothing;       // some tile has rows but no step
 };
 
-constexpr int kStarts = 1024;  // requests whose starts are kept in LDS
+constexpr int kStarts = kMaxDealt;  // their starts are kept in LDS
 template <int kThreads>
 struct DealLds {
   int64_t before[kThreads];  // steps of the tiles before a thread's
@@ -123,11 +123,9 @@ template <int kThreads, int kRows>
 __device__ inline Run find_run(const PromptArgs& a, const int32_t* __restrict__ lengths, const int32_t* __restrict__ start,
                                const int32_t* __restrict__ prefix, int w, DealLds<kThreads>& lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const bool few = a.requests <= kStarts;
-  if (few)
-    for (int i = threadIdx.x; i <= a.requests; i += kThreads) lds.starts[i] = start_of(a, start, i);
+  for (int i = threadIdx.x; i <= a.requests; i += kThreads) lds.starts[i] = start_of(a, start, i);
   __syncthreads();
-  const auto at = [&](int32_t r) { return few ? lds.starts[r] : start_of(a, start, r); };
+  const auto at = [&](int32_t r) { return lds.starts[r]; };
   const int32_t each = (a.tiles + kThreads - 1) / kThreads, x0 = threadIdx.x * each;
   int64_t mine = 0;
   bool nothing = false;
@@ -180,12 +178,10 @@ __device__ inline Run find_run(const PromptArgs& a, const int32_t* __restrict__ 
   for (int i = 0; i < kThreads / 64; ++i) owner += __popcll(__ballot(lds.before[64 * i + lane] <= off));
   off -= lds.before[owner];
   run.x = __builtin_amdgcn_readfirstlane(owner * each);
-  // starts from LDS are in order and in range, as they would be from memory
-  const int32_t* const from = few ? lds.starts : start;
-  int32_t r = request_of<kRows>(a, from, run.x);
+  int32_t r = request_of<kRows>(a, lds.starts, run.x);
   // ends before the last number; behind it only where starts go back and the counts differ
   for (; run.x < a.tiles; ++run.x) {
-    run.t = next_tile<kRows>(a, lengths, from, prefix, r, run.x);
+    run.t = next_tile<kRows>(a, lengths, lds.starts, prefix, r, run.x);
     r = run.t.r;
     if (off < run.t.count) break;
     off -= run.t.count;
