@@ -721,7 +721,8 @@ struct PartHead {
 // its K, 1 into the parts; the waves of a full chip end within 6 us of one another,
 // those that came to the memory first ahead. In 4 bits 217 us for the 192 sequences (5.3
 // TB/s); the long one of width 64, 77 us (3.9), is bound by instructions: two bytes of V a
-// lane and key. With kScored the 64 take 249 us, as without.
+// lane and key. With kScored the 64 take 249 us, as without; in 4
+// bits, where the vector unit is busy already, the 192 248 (cap) and 254 (cap and bias), the long one 107.
 template <int kType, int kDim, bool kScored>
 __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(
     const char* __restrict__ q, const char* __restrict__ k, const char* __restrict__ v,

@@ -77,10 +77,10 @@ __device__ inline int32_t request_of(const PromptArgs& a, const int32_t* __restr
 // neighbouring ones to a.groups workgroups, whatever the lengths (the GPU's), as the one-token
 // kernel does with its tiles. A tile that falls to several leaves a part in each, workgroup w's in
 // slot 2w if it began before and in slot 2w + 1 if it begins there: of each row kDim sums
-// and (m, l). With a workgroup for each tile instead, 8 frames of 1374 tokens over 10992
-// with 16 heads (768 tiles for the 512 workgroups that run at once) took 913 us, not 838.
-// Where tiles are two turns and more, dealing out costs: 10992 tokens at once 1307 us, not
-// 976 (neighbours then stand at different keys, and miss L2), 12 ragged prompts 400, not 378.
+// and (m, l). With a workgroup for each tile instead, 16 drafted tokens for each of 4
+// sequences of 10992 took 429 us, not 88, a frame of 1374 over 137400 with 16 heads 3079, not
+// 1048. Where tiles are many, dealing out costs: 10992 tokens at once 1309 us, not 982
+// (neighbours then stand at different keys, and miss L2), 12 ragged prompts 406, not 374.
 struct Cut {
   int32_t row, rows, first, h;
   int32_t from, to;
@@ -679,7 +679,7 @@ struct Rows {
   // present scores, so that the matrix cores and the vector unit work side by side; the
   // operands come from LDS two pairs of products ahead. (The compiler, left to itself or given
   // groups to interleave, puts the products of the wider form in a row: 1390 us for 10992
-// tokens at once, 1117 so, both without what the step does beside.)
+  // tokens at once, 1117 so, both without what the step does beside.)
   template <typename Beside>
   __device__ __forceinline__ void fused(const PromptArgs& a, lds_char* kb, lds_char* vb, const bf16x8 (&p)[2][2], float sc, bool changed, int32_t base, int hf,
                                         f32x16 (&z)[2], f32x16 (&next)[2], bf16x8 (&pn)[2][2], float (&sum)[2], Beside beside) {
@@ -832,9 +832,10 @@ struct Rows {
 // three steps before it is read. In 8 and 4 bits a step writes K t + 2 and V t, which were
 // asked for one step before, or four. 64 rows a wave: with 32 the LDS reads of K and V
 // alone would take as long as the products. 10992 tokens at once, 32 heads on 8 of 128 in
-// bf16: 976 us, 1015 TFLOP/s, where a library product reaches 1199; a step's 32 products
-// take 1024 of about 2200 cycles. 8 frames of 1374 tokens over 10992, 16 heads of 64 in 8
-// bits: 838 us, 665 TFLOP/s, bound by the vector unit.
+// bf16: 989 us, 1002 TFLOP/s, where a library product reaches 1199; a step's 32 products
+// take 1024 of about 2400 cycles. 8 frames of 1374 tokens over 10992, 16 heads of 64: in 8
+// bits 844 us, 660 TFLOP/s, bound by what goes beside a step's 16 products (156 vector and 107
+// scalar instructions: softmax, codes to bf16, lookups and addresses); in bf16 732, 760 TFLOP/s.
 constexpr int kWaves = 4;
 template <int kType, int kDim, int kScored>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kDim == 64 ? 2 : 1, kDim == 64 ? 2 : 1))) void
