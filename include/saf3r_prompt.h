@@ -64,8 +64,8 @@ saf3r_status saf3r_paged_attention_scored(const saf3r_page_layout* cache, const 
  * see everything, like a frame's. Scores may be changed as above (cap 0 and no slopes: as
  * they are). Query head h reads key-value head h / (q_heads / kv_heads).
  *   out = sum_j softmax(z)_j v_j,  lse = log(sum_j exp(z_j)) over the keys seen
- * A token that sees none gives zeros and lse -inf: so one whose request has fewer tokens
- * than new ones (p < 0), and one whose scores are all -inf. Keys whose page-table entry
+ * A token that sees none gives zeros and lse -inf: so one without a place, its request having
+ * fewer tokens than new ones (p < 0), that no prefix shows any, and one whose scores are all -inf. Keys whose page-table entry
  * lies outside [0, pages) are left out like masked ones. Tokens before token_start[0] and
  * from token_start[requests] on belong to nobody: their rows stay as they were. A request
  * that saf3r_page_tables refused kept its length: its new tokens count as its last ones, and

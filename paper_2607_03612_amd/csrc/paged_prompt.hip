@@ -556,6 +556,7 @@ struct Raw {
 
 struct Limits {
   int32_t place, below, from;
+  int32_t lost;  // see Rows::again
 };
 
 // A weight is 2^(z scale - m) with the product unrounded and m its rounded maximum: from here on
@@ -654,13 +655,13 @@ struct Rows {
     sum += y;
     return bf16x2{(__bf16)x, (__bf16)y};
   }
-  // kFar: from a maximum of 2^24 on scores are scaled first, so that the largest one's weight is 1.
-  template <bool kFar>
+  // kAgain: from a maximum of 2^24 on scores are scaled first, so that the largest one's weight is 1.
+  template <bool kAgain>
   __device__ __forceinline__ void weights(const f32x16 (&z)[2], const float (&nmu)[2], float sc, bf16x8 (&p)[2][2], float (&sum)[2]) const {
 #pragma unroll
     for (int tq = 0; tq < 2; ++tq) {
       sum[tq] = 0.0f;
-      const bool far = kFar && fabsf(nmu[tq]) >= kFarMaximum;
+      const bool far = kAgain && fabsf(nmu[tq]) >= kFarMaximum;
       const float by = far ? sc : 1.0f, then = far ? 1.0f : sc;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -668,7 +669,7 @@ struct Rows {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float z0 = z[tq][8 * u + 2 * e], z1 = z[tq][8 * u + 2 * e + 1];
-          x[e] = pair(kFar ? z0 * by : z0, kFar ? z1 * by : z1, kFar ? then : sc, nmu[tq], sum[tq]);
+          x[e] = pair(kAgain ? z0 * by : z0, kAgain ? z1 * by : z1, kAgain ? then : sc, nmu[tq], sum[tq]);
         }
         p[u][tq] = bf16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
       }
@@ -771,15 +772,15 @@ struct Rows {
   // The maximum moves only where a row's sum leaves [0, 2^12]: at its first key, where the
   // maximum is still none and the sum infinite or NaN, and where scores grew by much. A
   // row without a key so far keeps m = -inf and weights of 0; a row whose sum is in order
-  // keeps its maximum, whatever the others of the wave do.
-  template <bool kFar = false>
-  __device__ __forceinline__ void settle(const f32x16 (&z)[2], float sc, bf16x8 (&p)[2][2], float (&sum)[2]) {
-    if (__ballot(__float_as_uint(sum[0]) > 0x45800000u || __float_as_uint(sum[1]) > 0x45800000u)) {
+  // keeps its maximum, whatever the others of the wave do. kAgain: a lost row's follows every score.
+  template <bool kAgain = false>
+  __device__ __forceinline__ void settle(const f32x16 (&z)[2], float sc, bf16x8 (&p)[2][2], float (&sum)[2], int l32 = 0, const Limits* of = nullptr) {
+    if (kAgain || __ballot(__float_as_uint(sum[0]) > 0x45800000u || __float_as_uint(sum[1]) > 0x45800000u)) {
       float use[2];
 #pragma unroll
       for (int tq = 0; tq < 2; ++tq) {
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[tq]), __float_as_uint(sum[tq]), false, false);
-        const bool moves = max((uint32_t)both[0], (uint32_t)both[1]) > 0x45800000u;
+        const bool moves = max((uint32_t)both[0], (uint32_t)both[1]) > 0x45800000u || (kAgain && of[32 * tq + l32].lost);
         float top = z[tq][0];
         asm volatile("" : "+v"(top));  // the maximum is taken here only, not ahead of the branch
 #pragma unroll
@@ -789,10 +790,11 @@ struct Rows {
         nm[tq] = to;
         use[tq] = to == INFINITY ? 0.0f : to;
         l[tq] *= f;
+        if constexpr (kAgain) asm volatile("" : "+v"(l[tq]));  // rounded here, as behind the branch elsewhere
 #pragma unroll
         for (int c = 0; c < kC; ++c) o[c][tq] *= f;
       }
-      weights<kFar>(z, use, sc, p, sum);
+      weights<kAgain>(z, use, sc, p, sum);
     }
     l[0] += sum[0];
     l[1] += sum[1];
@@ -808,20 +810,22 @@ struct Rows {
         for (int e = 0; e < 16; ++e) o[c][tq][e] = 0.0f;
     }
   }
-  // Whether a row's weights may have left the exponent's range: its maximum is far, or was and
-  // left sums that are no numbers. A row without a key has neither.
-  __device__ __forceinline__ bool lost() const {
-    bool y = false;
+  // Whether a row's weights, or their products with V, may have left the exponent's range: the
+  // maximum is far, or sums are no numbers. A row without a key has neither.
+  __device__ __forceinline__ bool is_lost(int tq) const {
+    float none = l[tq] * 0.0f;
 #pragma unroll
-    for (int tq = 0; tq < 2; ++tq) {
-      float none = l[tq] * 0.0f;
+    for (int c = 0; c < kC; ++c)
 #pragma unroll
-      for (int c = 0; c < kC; ++c)
+      for (int e = 0; e < 16; ++e) none = fmaf(o[c][tq][e], 0.0f, none);
+    return none != 0.0f || (kScored == 0 && fabsf(nm[tq]) >= kFarMaximum && nm[tq] < INFINITY);
+  }
+  // Lost rows are noted; all sums from the start.
+  __device__ __forceinline__ void again(int l32, Limits* of) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) none = fmaf(o[c][tq][e], 0.0f, none);
-      y |= none != 0.0f || (fabsf(nm[tq]) >= kFarMaximum && nm[tq] < INFINITY);
-    }
-    return y;
+    for (int tq = 0; tq < 2; ++tq)
+      if (is_lost(tq)) of[32 * tq + l32].lost = 1;  // by either of its lanes
+    clear();
   }
 };
 
@@ -865,7 +869,7 @@ prompt_bf16_kernel(const char* __restrict__ q, const char* __restrict__ k, const
     const int head = h * b.group + row.head;
     w.slope[tq] = kScored && b.slopes ? b.slopes[head] * kLog2e : 0.0f;
     w.place[tq] = row.place;
-    if (hf == 0) limits[wave * 64 + tq * 32 + l32] = Limits{row.place, row.below, row.from};
+    if (hf == 0) limits[wave * 64 + tq * 32 + l32] = Limits{row.place, row.below, row.from, 0};
     const char* from = q + (head * b.q_head + row.token * b.q_token) * 2;
 #pragma unroll
     for (int s = 0; s < w.kS; ++s) w.q[tq][s] = *reinterpret_cast<const bf16x8*>(from + 32 * s + 16 * hf);
@@ -886,6 +890,9 @@ prompt_bf16_kernel(const char* __restrict__ q, const char* __restrict__ k, const
     all_from = __builtin_amdgcn_readfirstlane(high.from);
     all_place = __builtin_amdgcn_readfirstlane(low.place);
   }
+  const auto is_whole = [&](int32_t base, uint32_t absent) {
+    return absent == 0 && (base + kKeys <= all_below || (base >= all_from && base + kKeys - 1 <= all_place));
+  };
 
   const int32_t* const entries_row = table + (int64_t)t.r * a.max_pages;
   Entries entries{0x7fffffff - 64, -1};  // none yet
@@ -1058,7 +1065,7 @@ prompt_bf16_kernel(const char* __restrict__ q, const char* __restrict__ k, const
           if (product == 9) fetch(v, v_exp, spots[kAhead], r.v, r.ve);
         }
       };
-      const bool whole = absent == 0 && (base + kKeys <= all_below || (base >= all_from && base + kKeys - 1 <= all_place));
+      const bool whole = is_whole(base, absent);
       lds_char* const kb = kring[(P + 1) & 3];
       lds_char* const vb = vring[(P + 3) & 3];
       f32x16 next[2];
@@ -1106,34 +1113,47 @@ prompt_bf16_kernel(const char* __restrict__ q, const char* __restrict__ k, const
     w.read_v(rest == 0 ? vring[3] : rest == 1 ? vring[0] : rest == 2 ? vring[1] : vring[2], vw);
     w.mfma_pv(vw, p);
   }
-  // Scores that large are for the plainest walk, one step after the other; rows whose scores are
-  // not get the same bits again. (Told apart in each step's settle: 827 -> 855 us for 8 frames.)
-  if constexpr (kScored == 0) {
-    if (__syncthreads_or(w.lost())) {
-      w.clear();
-      for (int32_t x = lo; x < hi; ++x) {
-        const Y y = locate(x);
-        __syncthreads();
-        if constexpr (kType == 1) {
-          dma(k, y, kring[0]);
-          dma(v, y, vring[0]);
-        } else {
-          R r;
-          fetch_both(y, y, r);
-          put(r.k, r.ke, kring[0]);
-          put(r.v, r.ve, vring[0]);
-        }
-        sync(std::true_type{});
-        bf16x8 kw[W::kS], vw[2][W::kC];
-        w.read_k(kring[0], kw);
-        w.mfma_s(kw, z);
-        w.mask(z, y.base, lane, y.absent, limits + wave * 64);
-        float sum[2];
-        w.template weights<true>(z, w.nm, sc, p, sum);
-        w.template settle<true>(z, sc, p, sum);
-        w.read_v(vring[0], vw);
-        w.mfma_pv(vw, p);
+  // Lost rows take the plainest walk, one step after the other, in which their maximum follows
+  // every score; the tile's others get the same bits again. (Far maxima told apart in each step's
+  // settle: 827 -> 855 us for 8 frames.)
+  if (__syncthreads_or(w.is_lost(0) || w.is_lost(1))) {
+    w.again(l32, limits + wave * 64);
+    for (int32_t x = lo; x < hi; ++x) {
+      const Y y = locate(x);
+      __syncthreads();
+      if constexpr (kType == 1) {
+        dma(k, y, kring[0]);
+        dma(v, y, vring[0]);
+      } else {
+        R r;
+        fetch_both(y, y, r);
+        put(r.k, r.ke, kring[0]);
+        put(r.v, r.ve, vring[0]);
       }
+      sync(std::true_type{});
+      bf16x8 kw[W::kS], vw[2][W::kC];
+      w.read_k(kring[0], kw);
+      w.mfma_s(kw, z);
+      if constexpr (kScored) {
+        const bool brief = kScored == 2 && !a.far_cap && is_whole(y.base, y.absent);
+#pragma unroll
+        for (int tq = 0; tq < 2; ++tq) {
+          const float far = w.far_of(tq, y.base, hf);
+          if (brief) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[tq][e] = w.lowered(w.capped(a, z[tq][e]), tq, e, far);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[tq][e] = w.change(a, z[tq][e], tq, e, far);
+          }
+        }
+      }
+      w.mask(z, y.base, lane, y.absent, limits + wave * 64);
+      float sum[2];
+      w.template weights<true>(z, w.nm, sc, p, sum);
+      w.template settle<true>(z, sc, p, sum, l32, limits + wave * 64);
+      w.read_v(vring[0], vw);
+      w.mfma_pv(vw, p);
     }
   }
 

@@ -225,3 +225,49 @@ def test_large_caps(gpu_lib, dtype, D, cap, size, kind):
         uncapped = Q.attend(*args, 0.0, slopes)
         want = (*want[:2], 1.1 * uncapped[2], 1.1 * uncapped[3], want[4])
     check(out, lse, want, dtype, 0 if dtype == "f32" else 8, n)
+
+
+@pytest.mark.parametrize("dtype", ALL)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap,kind", [(0.0, None), (40.0, None), (3000.0, None), (0.0, "falling"), (40.0, "falling")])
+def test_large_values_behind_growing_scores(gpu_lib, dtype, D, cap, kind):
+    """A value near the largest number whose score is 7 over those before: its product with a weight is no larger than it is."""
+    import paper_2607_03612_amd as P
+
+    n, T = 200, 60
+    k = np.zeros((n, 1, D))
+    v = np.random.default_rng(D).standard_normal((n, 1, D))
+    k[150] = 1.0
+    v[150] = 1.5 * 2.0 ** 124
+    kv, exps, table, k, v = held(dtype, k, v)
+    q = torch.full((2, T, D), 7.0 / D, dtype=wide(dtype), device=DEV)
+    q[1] = 0.5 / D
+    place = np.arange(n - T, n)
+    slopes = None if kind is None else slopes_of(2, kind) * 0.01
+    more = dict(scale=1.0, cap=cap, slopes=slopes, want_lse=True)
+    want = Q.attend(q.double().cpu().numpy(), place, k, v, 1.0, Q.seen(n, place), cap, None if kind is None else slopes.double().cpu().numpy())
+    out, lse = P.prompt_attention(q, *kv, table, ints([n]), ints([0, T]), *exps, **more)
+    check(out, lse, want, dtype, 0 if dtype == "f32" else 8, n)
+    out, lse = P.paged_attention(q[:, T - 1:], *kv, table, ints([n]), *exps, **more)
+    check(out, lse, tuple(x[:, -1:] for x in want), dtype, 0 if dtype == "f32" else 16, n)
+
+
+@pytest.mark.parametrize("dtype", ALL)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap,kind", [(0.0, None), (9.0, None), (3000.0, None), (0.0, "falling"), (9.0, "falling")])
+def test_rows_that_are_walked_again_leave_the_others(gpu_lib, dtype, D, cap, kind):
+    """A query that is NaN, far scores: neither changes a bit of its neighbours', in tiles that one workgroup has whole and in
+    ones that several share, with masks by prefix and window."""
+    import paper_2607_03612_amd as P
+
+    c = Cache(8, dtype, [900, 300], 2, D, 16)
+    q = queries(9, 8, 150, D, dtype, scale=3.0)
+    more = dict(prefix=ints([64, 5]), anchor=40, window=500, cap=cap, slopes=None if kind is None else slopes_of(8, kind), want_lse=True)
+    want, want_lse = P.prompt_attention(q, *c.kv, c.table, c.lengths, ints([0, 100, 150]), *c.exps, **more)
+    q[2, 40, 3], q[5, 149, 0] = float("nan"), float("inf")
+    q[7, 99] *= 2.0 ** 40
+    out, lse = P.prompt_attention(q, *c.kv, c.table, c.lengths, ints([0, 100, 150]), *c.exps, **more)
+    assert bool(out[2, 40].isnan().all()) and bool(lse[2, 40].isnan()) and bool(out[7, 99].isfinite().all())
+    for h, t in ((2, 40), (5, 149), (7, 99)):
+        out[h, t], lse[h, t] = want[h, t], want_lse[h, t]
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
